@@ -176,7 +176,7 @@ def _codes(x):
     b = x.float().reshape(*x.shape[:-1], x.shape[-1] // 32, 32)
     amax = b.abs().amax(-1)
     byte = ((amax.view(torch.int32) + 0x1FFFFF) >> 23) - 2  # the exponent of amax, one more above 1.75 times a power of two
-    byte = torch.where(amax.isfinite(), byte.clamp(1, 253), 255)
+    byte = torch.where(amax.isfinite(), byte.clamp(1, 252), 255)
     a = torch.ldexp(b.abs(), (127 - byte)[..., None])
     # to the nearest element, ties to the one with an even code
     code = (a > 0.25).int() + (a >= 0.75).int() + (a > 1.25).int() + (a >= 1.75).int() + (a > 2.5).int() + (a >= 3.5).int() + (a > 5.0).int()
@@ -405,7 +405,7 @@ def _nearest(x):
     b = x.reshape(-1, 32)
     amax = b.abs().max(1).values
     m, e = torch.frexp(amax)  # amax = m 2^e, m in [0.5, 1)
-    step = torch.pow(2.0, ((e - 3) + (m > 0.875).int()).clamp(min=-126).double())[:, None]
+    step = torch.pow(2.0, ((e - 3) + (m > 0.875).int()).clamp(-126, 125).double())[:, None]
     grid = torch.tensor(GRID, dtype=torch.float64, device=x.device)
     a = b.abs() / step
     lower = (torch.searchsorted(grid, a.contiguous(), right=True) - 1).clamp(max=6)
