@@ -5,7 +5,7 @@ The functions below say through ctypes what each call takes; at the end of the m
 forms are not there, or were built for another torch, the functions stay what they are: the same calls, a few microseconds of
 host time longer each.
 
-Every function has the name and argument order of its C entry point (include/dllava.h); tensors are
+Every function has the name and argument order of its C entry point (include/dllava.h, include/dllava_mx.h); tensors are
 torch tensors used purely as device buffers (data_ptr), and the stream defaults to torch's current
 stream.  A non-zero status raises DllavaError with the library's message.  Nothing here computes:
 if the shared library is missing the import fails.
@@ -23,6 +23,7 @@ import torch
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "lib", "libdllava.so")
 
 F32, BF16 = 0, 1
+MX = 2  # of a cache whose pages are in 4 bits
 MODE_TOPK, MODE_THRESHOLD, MODE_THRESHOLD_KEEP_LAST = 0, 1, 2
 LAUNCH_DECODE_WAVES, LAUNCH_DECODE_SPLITS, LAUNCH_PREFILL_WAVES, LAUNCH_SCORE_TILE, LAUNCH_QKV_TILE, LAUNCH_PREFILL_BLOCKS = 0, 1, 2, 3, 4, 5
 LAUNCH_SELECT_LAUNCHES = 6
@@ -127,6 +128,27 @@ def _load() -> C.CDLL:
     lib.dllava_rms_norm.argtypes = [vp, i64, i64, i64, vp, f32, vp, i64, C.c_int, vp]
     lib.dllava_span_attn.restype = C.c_int
     lib.dllava_span_attn.argtypes = [vp, vp, vp, i32, vp, i64, i32, i32, f32, vp, C.c_int, vp]
+    cache = C.POINTER(_KvCache)
+    lib.dllava_mx_bytes.restype = sz
+    lib.dllava_mx_bytes.argtypes = [i64, i64]
+    lib.dllava_mx_quantize.restype = C.c_int
+    lib.dllava_mx_quantize.argtypes = [vp, i64, i64, i64, vp, sz, C.c_int, vp]
+    lib.dllava_mx_dequantize.restype = C.c_int
+    lib.dllava_mx_dequantize.argtypes = [vp, sz, i64, i64, vp, i64, C.c_int, vp]
+    lib.dllava_mx_linear.restype = C.c_int
+    lib.dllava_mx_linear.argtypes = [vp, sz, i64, i64, vp, sz, vp, i64, C.c_int, vp, vp, i64, C.c_int, vp]
+    lib.dllava_mx_linear_few.restype = C.c_int
+    lib.dllava_mx_linear_few.argtypes = [vp, i64, i64, i64, vp, sz, vp, i64, C.c_int, vp, vp, i64, C.c_int, vp]
+    lib.dllava_mx_cache_store.restype = C.c_int
+    lib.dllava_mx_cache_store.argtypes = [vp, vp, i64, i32, vp, vp, i64, vp, vp, cache, vp, C.c_int, vp]
+    lib.dllava_mx_cache_load.restype = C.c_int
+    lib.dllava_mx_cache_load.argtypes = [cache, i32, vp, vp, i64, vp, vp, i64, C.c_int, vp]
+    lib.dllava_mx_decode_attn_append.restype = C.c_int
+    lib.dllava_mx_decode_attn_append.argtypes = [vp, vp, vp, i32, i32, vp, f32, vp, cache, f32, vp, vp, vp, vp, sz, vp]
+    lib.dllava_mx_decode_workspace.restype = sz
+    lib.dllava_mx_decode_workspace.argtypes = [i32, i32, i32, i32, i32]
+    lib.dllava_group_prefill_attn.restype = C.c_int
+    lib.dllava_group_prefill_attn.argtypes = [vp, i64, vp, vp, i64, i32, vp, i64, i32, i32, i32, f32, vp, C.c_int, vp]
     return lib
 
 
@@ -139,6 +161,9 @@ EXPORTS = ("dllava_version", "dllava_last_error", "dllava_set_launch_override", 
            "dllava_masked_attn", "dllava_masked_attn_workspace", "dllava_compact", "dllava_rms_norm", "dllava_linear_few",
            "dllava_linear_few_workspace", "dllava_rope", "dllava_qkv_few", "dllava_gated_few",
            "dllava_decode_proj_workspace")
+# include/dllava_mx.h: 4 bits, grouped heads
+EXPORTS_MX = ("dllava_mx_bytes", "dllava_mx_quantize", "dllava_mx_dequantize", "dllava_mx_linear", "dllava_mx_linear_few", "dllava_mx_cache_store",
+              "dllava_mx_cache_load", "dllava_mx_decode_attn_append", "dllava_mx_decode_workspace", "dllava_group_prefill_attn")
 
 
 def lib() -> C.CDLL:
@@ -178,17 +203,25 @@ def _ws(workspace: Optional[torch.Tensor]):
 
 
 class KVCache:
-    """Host-side descriptor (dllava_kv_cache) over caller-owned device tensors."""
+    """Host-side descriptor (dllava_kv_cache) over caller-owned device tensors.
+
+    pages: [n_pages, 2, H, 16, Dh] float32 or bfloat16, or, for a cache in 4 bits (include/dllava_mx.h), [n_pages, H, 17 * Dh] uint8.
+    """
 
     def __init__(self, pages: torch.Tensor, block_table: torch.Tensor, cache_len: torch.Tensor):
-        n_pages, two, H, ps, Dh = pages.shape
+        if pages.dtype == torch.uint8:
+            n_pages, H, page_bytes = pages.shape
+            two, ps, Dh = 2, PAGE_SIZE, page_bytes // 17
+            assert page_bytes == 17 * Dh
+        else:
+            n_pages, two, H, ps, Dh = pages.shape
         assert two == 2 and pages.is_contiguous() and block_table.is_contiguous()
         assert block_table.dtype == torch.int32 and cache_len.dtype == torch.int32
         self.pages, self.block_table, self.cache_len = pages, block_table, cache_len
         self.H, self.Dh, self.page_size = H, Dh, ps
         self.B, self.max_pages_per_seq = block_table.shape
         self.c = _KvCache(pages.data_ptr(), block_table.data_ptr(), cache_len.data_ptr(), n_pages,
-                          self.max_pages_per_seq, ps, H, Dh, dtype_code(pages.dtype))
+                          self.max_pages_per_seq, ps, H, Dh, MX if pages.dtype == torch.uint8 else dtype_code(pages.dtype))
 
     @property
     def ref(self):
@@ -376,6 +409,55 @@ def dllava_decode_attn_append_static(q, k_new, v_new, B, logits, threshold, keep
                                                  _p(err_flag), _stream(stream)))
 
 
+def dllava_mx_bytes(M: int, K: int) -> int:
+    return _lib.dllava_mx_bytes(M, K)
+
+
+def dllava_mx_quantize(x, ldx, M, K, packed, dtype, stream=None) -> None:
+    pp, pb = _ws(packed)
+    _check(_lib.dllava_mx_quantize(_p(x), ldx, M, K, pp, pb, dtype, _stream(stream)))
+
+
+def dllava_mx_dequantize(packed, M, K, y, ldy, dtype, stream=None) -> None:
+    pp, pb = _ws(packed)
+    _check(_lib.dllava_mx_dequantize(pp, pb, M, K, _p(y), ldy, dtype, _stream(stream)))
+
+
+def dllava_mx_linear(xq, M, K, Wq, bias, N, act, residual, y, ldy, dtype, stream=None) -> None:
+    xp, xb = _ws(xq)
+    wp, wb = _ws(Wq)
+    _check(_lib.dllava_mx_linear(xp, xb, M, K, wp, wb, _p(bias), N, act, _p(residual), _p(y), ldy, dtype, _stream(stream)))
+
+
+def dllava_mx_linear_few(x, ldx, M, K, Wq, bias, N, act, residual, y, ldy, dtype, stream=None) -> None:
+    wp, wb = _ws(Wq)
+    _check(_lib.dllava_mx_linear_few(_p(x), ldx, M, K, wp, wb, _p(bias), N, act, _p(residual), _p(y), ldy, dtype, _stream(stream)))
+
+
+def dllava_mx_cache_store(K, V, ldkv, B, off, start, rows, src_off, src_idx, cache: KVCache, err_flag, dtype, stream=None) -> None:
+    _check(_lib.dllava_mx_cache_store(_p(K), _p(V), ldkv, B, _p(off), _p(start), rows, _p(src_off), _p(src_idx), cache.ref, _p(err_flag), dtype,
+                                      _stream(stream)))
+
+
+def dllava_mx_cache_load(cache: KVCache, B, off, start, rows, K, V, ldkv, dtype, stream=None) -> None:
+    _check(_lib.dllava_mx_cache_load(cache.ref, B, _p(off), _p(start), rows, _p(K), _p(V), ldkv, dtype, _stream(stream)))
+
+
+def dllava_mx_decode_workspace(B: int, Hq: int, H: int, Dh: int, max_pages_per_seq: int) -> int:
+    return _lib.dllava_mx_decode_workspace(B, Hq, H, Dh, max_pages_per_seq)
+
+
+def dllava_mx_decode_attn_append(q, k_new, v_new, B, Hq, logits, threshold, keep_override, cache: KVCache, scale, o, keep_out, err_flag, workspace,
+                                 stream=None) -> None:
+    wp, wb = _ws(workspace)
+    _check(_lib.dllava_mx_decode_attn_append(_p(q), _p(k_new), _p(v_new), B, Hq, _p(logits), threshold, _p(keep_override), cache.ref, scale, _p(o),
+                                             _p(keep_out), _p(err_flag), wp, wb, _stream(stream)))
+
+
+def dllava_group_prefill_attn(Q, ldq, K, V, ldkv, B, off, rows, Hq, Hkv, Dh, scale, O, dtype, stream=None) -> None:
+    _check(_lib.dllava_group_prefill_attn(_p(Q), ldq, _p(K), _p(V), ldkv, B, _p(off), rows, Hq, Hkv, Dh, scale, _p(O), dtype, _stream(stream)))
+
+
 def _bind_native() -> None:
     torch_here = f"{torch.__version__} {torch.version.git_version}"
     try:
@@ -387,7 +469,7 @@ def _bind_native() -> None:
                       "(`python -m paper_2412_00876_amd.build` builds the native forms)", RuntimeWarning, stacklevel=2)
         return
     _calls.init(KVCache, Predictor, _check, torch.cuda.current_device, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
-    for name in EXPORTS:
+    for name in EXPORTS + EXPORTS_MX:
         python = globals().get(name)
         if python is None:
             continue

@@ -435,7 +435,8 @@ __device__ __forceinline__ void finish(State<DH>& T, const Probs& P) {
 
 // Paged: causal, keys and values in the cache's pages.  Rows: causal, in rows.  Full: every query sees all keys of its sequence.
 // Masked: causal, keys hidden by key words but from their own query.  Words: the same without counts and list of the visible keys.
-enum class Mode { Paged, Rows, Full, Masked, Words };
+// Group: causal, in rows, several query heads to a head of K and V, rows of any stride.
+enum class Mode { Paged, Rows, Full, Masked, Words, Group };
 
 // One work item = (sequence, head, tile of NWQ*32 query rows).  Blocks are PERSISTENT: the launch holds as many blocks as
 // fit the chip at once (slots), block p takes every slots-th item and walks their key tiles as ONE stream: the tile
@@ -446,7 +447,7 @@ enum class Mode { Paged, Rows, Full, Masked, Words };
 // with its tile index, so every block takes its longest items first and the launch ends with the shortest ones.
 template <int DH, int NWQ, Mode MODE>
 __device__ __forceinline__ void attend_items(const PrefillArgs& args) {
-  constexpr bool kFull = MODE == Mode::Full, kList = MODE == Mode::Masked, kMasks = kList || MODE == Mode::Words;
+  constexpr bool kFull = MODE == Mode::Full, kList = MODE == Mode::Masked, kMasks = kList || MODE == Mode::Words, kGroup = MODE == Mode::Group;
   // the arguments as locals (the closures below then capture plain values, which the compiler keeps in registers)
   const int aB = args.B;
   const float aScale = args.scale_log2;
@@ -493,7 +494,7 @@ __device__ __forceinline__ void attend_items(const PrefillArgs& args) {
   const ConstU32 kw_c = (ConstU32)args.key_words;
   constexpr bool paged = MODE == Mode::Paged;
   const int step_blocks = static_cast<int>(gridDim.x);
-  const uint32_t row_bytes = paged ? kRowBytes : static_cast<uint32_t>(H) * kRowBytes;
+  const uint32_t row_bytes = kGroup ? args.kv_row_bytes : (paged ? kRowBytes : static_cast<uint32_t>(H) * kRowBytes);
 
   auto uniform = [](int v) DLLAVA_INLINE { return __builtin_amdgcn_readfirstlane(v); };  // said to the compiler where it cannot see it
   // Which (sequence, query tile) is item k?  With at most 64 sequences every wave keeps the sequences' offsets in
@@ -614,7 +615,8 @@ __device__ __forceinline__ void attend_items(const PrefillArgs& args) {
       const int rr = D::kRowsPerLoad * i + l / kChunks, pc = l % kChunks;
       int q = (tile < 0 ? 0 : tile * 32) + rr;
       if (q >= it.n) q = it.n - 1;
-      const bf16_t* src = Qp + (static_cast<size_t>(it.r0 + q) * heads + it.h) * DH + 8 * (pc ^ D::k_swizzle(rr));
+      const bf16_t* src = Qp + (kGroup ? static_cast<size_t>(it.r0 + q) * (arg(&PrefillArgs::q_row_bytes) / 2) + static_cast<size_t>(it.h) * DH
+                                       : (static_cast<size_t>(it.r0 + q) * heads + it.h) * DH) + 8 * (pc ^ D::k_swizzle(rr));
       load_to_lds(reinterpret_cast<const char*>(src), lds_address(myQ) + i * (kWave * 16));
     }
   };
@@ -725,7 +727,7 @@ __device__ __forceinline__ void attend_items(const PrefillArgs& args) {
     P.b = uniform(P.b), P.h = uniform(P.h), P.tile = uniform(P.tile), P.r0 = uniform(P.r0), P.n = uniform(P.n);
     lastP = last_key_of(P);
     baseP = paged ? static_cast<const char*>(args.pages) + static_cast<int64_t>(P.h) * (kPage * kRowBytes)
-                  : static_cast<const char*>(arg(&PrefillArgs::K)) + static_cast<int64_t>(P.r0) * row_bytes + P.h * kRowBytes;
+                  : static_cast<const char*>(arg(&PrefillArgs::K)) + static_cast<int64_t>(P.r0) * row_bytes + (kGroup ? P.h / arg(&PrefillArgs::group) : P.h) * kRowBytes;
     tP = 0;
     if constexpr (kMasks) {
       leftP = kList ? uniform(P.seen) : -1;

@@ -22,6 +22,7 @@
 #include <utility>
 
 #include "dllava.h"
+#include "dllava_mx.h"
 
 namespace {
 
@@ -196,6 +197,14 @@ const Kind kKinds[] = {
     kind<decltype(&dllava_rope)>("dllava_rope"),
     kind<decltype(&dllava_qkv_few)>("dllava_qkv_few"),
     kind<decltype(&dllava_gated_few)>("dllava_gated_few"),
+    kind<decltype(&dllava_mx_quantize)>("dllava_mx_quantize"),
+    kind<decltype(&dllava_mx_dequantize)>("dllava_mx_dequantize"),
+    kind<decltype(&dllava_mx_linear)>("dllava_mx_linear"),
+    kind<decltype(&dllava_mx_linear_few)>("dllava_mx_linear_few"),
+    kind<decltype(&dllava_mx_cache_store)>("dllava_mx_cache_store"),
+    kind<decltype(&dllava_mx_cache_load)>("dllava_mx_cache_load"),
+    kind<decltype(&dllava_mx_decode_attn_append)>("dllava_mx_decode_attn_append"),
+    kind<decltype(&dllava_group_prefill_attn)>("dllava_group_prefill_attn"),
 };
 
 // ---- the callable -----------------------------------------------------------------------------------------------------------

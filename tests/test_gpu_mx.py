@@ -1,0 +1,200 @@
+"""Rows, weights and linear layers in microscaled 4-bit floating point against the oracle (float64): bytes and read values exactly,
+results of the products to their rounding.
+
+Tolerance of a result y of a product over K: its own rounding to bfloat16, half a step, 2^-8 |y|; and float32 sums of K exact
+products, the bias and the residual: each of the additions, and the few roundings of an activation, is off by at most 2^-23 of the
+partial sums' magnitude A, together (K + 8) 2^-23 A (the oracle returns A, times the activation's slope)."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import paper_2412_00876_amd as P
+from oracle import mx_ref as R
+
+DEV = "cuda:0"
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+    return t if dtype is None else t.to(dtype)
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def rows_of(rs, M, K, dtype, ld=None):
+    """Rows with values of many magnitudes, and what lies beside them NaN."""
+    x = torch.full((M, ld or K), float("nan"), dtype=dtype, device=DEV)
+    x[:, :K] = dev(rs.standard_normal((M, K)) * np.exp2(rs.integers(-6, 7, (M, 1))))
+    return x
+
+
+def packed(rs, M, K, scale=1.0):
+    """Packed random rows on the device, and their values."""
+    c, s = R.quantize((rs.standard_normal((M, K)) * scale).astype(np.float32))
+    return dev(R.pack(c, s)), R.dequantize(c, s)
+
+
+CODE = {torch.float32: P.F32, torch.bfloat16: P.BF16}
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,K,ld", [(1, 32, 32), (2, 64, 72), (17, 96, 104), (16, 512, 512), (33, 544, 1088), (5, 11008, 11008), (130, 1376, 1376)])
+def test_quantize_and_back(M, K, ld, dtype):
+    rs = np.random.default_rng(M * K)
+    x = rows_of(rs, M, K, dtype, ld)
+    n = P.dllava_mx_bytes(M, K)
+    q = torch.full((n + 256,), 0xA5, dtype=torch.uint8, device=DEV)
+    P.dllava_mx_quantize(x, ld, M, K, q, CODE[dtype])
+    c, s = R.quantize(f64(x[:, :K]))
+    assert np.array_equal(q[:n].cpu().numpy(), R.pack(c, s))
+    assert (q[n:] == 0xA5).all()
+    for out in (torch.float32, torch.bfloat16):
+        y = torch.full((M, ld), 7.0, dtype=out, device=DEV)
+        P.dllava_mx_dequantize(q, M, K, y, ld, CODE[out])
+        assert np.array_equal(f64(y[:, :K]), R.dequantize(c, s)) and (y[:, K:] == 7.0).all()
+
+
+def test_quantize_special_values():
+    f = lambda *bits: np.array(bits, np.uint32).view(np.float32)
+    rows = [np.zeros(32, np.float32), -np.zeros(32, np.float32), np.full(32, 3.4e38, np.float32)]
+    rows += [np.resize(f(b), 32) for b in (1, 0x7FFFFF, 0x800000, 0x00800001, 0x01000000, 0x7F7FFFFF, 0x7F600000, 0x7F600001)]  # smallest .. largest
+    ties = np.array([0, .25, .5, .75, 1, 1.25, 1.5, 1.75, 2, 2.5, 3, 3.5, 4, 5, 6, 7], np.float32)
+    for e in (-149, -126, -60, 0, 60, 120):
+        t = np.ldexp(ties, e).astype(np.float32)
+        rows += [np.concatenate([t, -t]), np.concatenate([np.nextafter(t, np.float32(np.inf)), np.nextafter(t, np.float32(0))])]
+    rows += [np.r_[np.float32(1.75 * 2.0 ** e), np.full(31, 2.0 ** e, np.float32)].astype(np.float32) for e in (-10, 3)]
+    rows += [np.r_[np.nextafter(np.float32(1.75), np.float32(2)), np.full(31, 0.1, np.float32)].astype(np.float32)]
+    for bad in (np.inf, -np.inf, np.nan):
+        r = np.linspace(-3, 3, 32).astype(np.float32)
+        r[7] = bad
+        rows.append(r)
+    x = np.stack(rows)
+    for dtype in (torch.float32, torch.bfloat16):
+        xd = dev(x).to(dtype)
+        q = torch.empty(P.dllava_mx_bytes(len(x), 32), dtype=torch.uint8, device=DEV)
+        P.dllava_mx_quantize(xd, 32, len(x), 32, q, CODE[dtype])
+        y = torch.empty((len(x), 32), dtype=torch.float32, device=DEV)
+        P.dllava_mx_dequantize(q, len(x), 32, y, 32, P.F32)
+        xv = xd.float().cpu().numpy()
+        c, s = R.quantize(xv)
+        want, got = R.dequantize(c, s), y.cpu().numpy()
+        finite = np.isfinite(xv).all(1)
+        assert np.array_equal(got[finite], want[finite]) and np.array_equal(np.signbit(got[finite]), np.signbit(xv[finite]))
+        assert np.isnan(got[~finite]).all()
+
+
+def test_every_scale_byte_and_code_is_read():
+    c = np.tile(np.arange(16, dtype=np.uint8), (256, 2))
+    s = np.arange(256, dtype=np.uint8)[:, None]
+    y = torch.empty((256, 32), dtype=torch.float32, device=DEV)
+    P.dllava_mx_dequantize(dev(R.pack(c, s)), 256, 32, y, 32, P.F32)
+    got, want = f64(y), R.dequantize(c, s)
+    assert np.isnan(got[255]).all()
+    want = np.where(np.abs(want) >= 2.0 ** 128, np.sign(want) * np.inf, want)   # 4 * 2^126 is out of range
+    assert np.array_equal(got[:255], want[:255])
+
+
+LINEAR = [(1, 32, 8), (15, 96, 24), (64, 512, 264), (65, 544, 520), (200, 1376, 136), (257, 4096, 72), (130, 11008, 40), (300, 1024, 1032)]
+
+
+def check_linear(y, x, W, bias, act, residual, K):
+    want, mag = R.linear(x, W, bias, act, residual)
+    tol = 2.0 ** -8 * np.abs(want) + (K + 8) * 2.0 ** -23 * mag
+    bad = ~(np.abs(f64(y) - want) <= tol)
+    assert not bad.any(), (bad.sum(), np.argwhere(bad)[:5], np.abs(f64(y) - want).max())
+
+
+@pytest.mark.parametrize("act,bias,residual", [(0, False, False), (0, True, True), (1, True, False), (1, False, True), (2, True, True)])
+@pytest.mark.parametrize("M,K,N", LINEAR)
+def test_linear(M, K, N, act, bias, residual):
+    rs = np.random.default_rng(M + K + N + act)
+    xq, x = packed(rs, M, K)
+    Wq, W = packed(rs, N, K, K ** -0.5)
+    b = dev(rs.standard_normal(N).astype(np.float32)) if bias else None
+    ldy = N + 16
+    y = torch.full((M, ldy), 5.0, dtype=torch.bfloat16, device=DEV)
+    r = None
+    if residual:
+        y[:, :N] = dev(rs.standard_normal((M, N))).bfloat16()
+        r = y.clone()
+    P.dllava_mx_linear(xq, M, K, Wq, b, N, act, r, y, ldy, P.BF16)
+    check_linear(y[:, :N], x, W, None if b is None else f64(b), act, None if r is None else f64(r[:, :N]), K)
+    assert (y[:, N:] == 5.0).all()
+    if residual:                                            # in place: the same bits
+        P.dllava_mx_linear(xq, M, K, Wq, b, N, act, r, r, ldy, P.BF16)
+        assert torch.equal(r, y)
+
+
+@pytest.mark.parametrize("act,bias,residual", [(0, False, False), (0, True, True), (1, True, False), (2, False, True)])
+@pytest.mark.parametrize("M", [1, 2, 16, 17, 33, 49, 64])
+@pytest.mark.parametrize("K,N", [(32, 8), (96, 24), (1376, 520), (4096, 264), (11008, 40), (512, 8200), (96, 16400)])
+def test_linear_few(M, K, N, act, bias, residual):
+    rs = np.random.default_rng(M + K + N + act)
+    x = rows_of(rs, M, K, torch.bfloat16, K + 8)            # NaN behind the rows' ends
+    Wq, W = packed(rs, N, K, K ** -0.5)
+    b = dev(rs.standard_normal(N).astype(np.float32)) if bias else None
+    y = torch.full((M, N + 8), 5.0, dtype=torch.bfloat16, device=DEV)
+    r = None
+    if residual:
+        y[:, :N] = dev(rs.standard_normal((M, N))).bfloat16()
+        r = y.clone()
+    P.dllava_mx_linear_few(x, K + 8, M, K, Wq, b, N, act, r, y, N + 8, P.BF16)
+    check_linear(y[:, :N], f64(x[:, :K]), W, None if b is None else f64(b), act, None if r is None else f64(r[:, :N]), K)
+    assert (y[:, N:] == 5.0).all()
+    if residual:
+        P.dllava_mx_linear_few(x, K + 8, M, K, Wq, b, N, act, r, r, N + 8, P.BF16)
+        assert torch.equal(r, y)
+
+
+def test_nan_stays_in_its_row():
+    """A block with an infinity makes its row NaN, in the rows' and in the weights' part, and no other."""
+    rs = np.random.default_rng(3)
+    M, K, N = 70, 544, 72
+    x, W = rs.standard_normal((M, K)).astype(np.float32), rs.standard_normal((N, K)).astype(np.float32)
+    x[33, 543], W[71, 0] = np.inf, np.nan
+    xq, Wq = dev(R.pack(*R.quantize(x))), dev(R.pack(*R.quantize(W)))
+    y = torch.empty((M, N), dtype=torch.bfloat16, device=DEV)
+    P.dllava_mx_linear(xq, M, K, Wq, None, N, 0, None, y, N, P.BF16)
+    want = np.zeros((M, N), bool)
+    want[33], want[:, 71] = True, True
+    assert np.array_equal(np.isnan(f64(y)), want)
+    few = torch.empty((40, N), dtype=torch.bfloat16, device=DEV)
+    P.dllava_mx_linear_few(dev(x).bfloat16(), K, 40, K, Wq, None, N, 0, None, few, N, P.BF16)
+    assert np.array_equal(~np.isfinite(f64(few)), want[:40])
+
+
+def test_another_stream_and_a_replayed_graph():
+    rs = np.random.default_rng(4)
+    M, K, N = 70, 1376, 264
+    x = rows_of(rs, M, K, torch.bfloat16)
+    Wq, W = packed(rs, N, K, K ** -0.5)
+    q = torch.empty(P.dllava_mx_bytes(M, K), dtype=torch.uint8, device=DEV)
+    y, few = torch.zeros((M, N), dtype=torch.bfloat16, device=DEV), torch.zeros((37, N), dtype=torch.bfloat16, device=DEV)
+
+    def call():
+        P.dllava_mx_quantize(x, K, M, K, q, P.BF16)
+        P.dllava_mx_linear(q, M, K, Wq, None, N, 0, None, y, N, P.BF16)
+        P.dllava_mx_linear_few(x, K, 37, K, Wq, None, N, 1, None, few, N, P.BF16)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for seed in range(3):
+        x.copy_(rows_of(np.random.default_rng(50 + seed), M, K, torch.bfloat16))
+        call()
+        eager = y.clone(), few.clone()
+        y.zero_(), few.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, eager[0]) and torch.equal(few, eager[1])
+        c, s = R.quantize(f64(x))
+        check_linear(y, R.dequantize(c, s), W, None, 0, None, K)

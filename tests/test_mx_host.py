@@ -1,0 +1,202 @@
+"""Without a GPU: the oracle of the 4-bit format against its definition, and what the calls of include/dllava_mx.h refuse on the host,
+through ctypes and through the binding's native forms."""
+import ctypes as C
+import inspect
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2412_00876_amd.binding as b
+from oracle import mx_ref as R
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+EINVAL, ENULL, ESHAPE, EDTYPE, ECAPACITY, EWORKSPACE = -1, -2, -3, -4, -5, -6
+
+
+# ---- the oracle ---------------------------------------------------------------------------------------------------------------------
+def test_rounding_by_hand():
+    x = np.zeros((4, 32))
+    x[0, :9] = [6, .25, .26, .75, 1.25, 1.75, 2.5, 3.5, 5]    # scale 1: ties to even codes
+    x[1, :4] = [7, -7, 5.1, 0.2]                              # 1.75 * 4: not more, so scale 1, and seven saturates
+    x[2, :3] = [7.0001, 6, 1]                                 # more: scale 2
+    x[3, :2] = [np.inf, 1]
+    c, s = R.quantize(x)
+    assert s[:, 0].tolist() == [127, 127, 128, 255]
+    v = R.dequantize(c, s)
+    assert v[0, :9].tolist() == [6, 0, .5, 1, 1, 2, 2, 4, 4]
+    assert v[1, :4].tolist() == [6, -6, 6, 0] and v[2, :3].tolist() == [8, 6, 1] and np.isnan(v[3]).all()
+
+
+def test_rounding_is_nearest_everywhere():
+    rs = np.random.default_rng(0)
+    x = rs.standard_normal((2000, 32)) * np.exp2(rs.integers(-150, 120, (2000, 1)))
+    c, s = R.quantize(x)
+    v = R.dequantize(c, s)
+    step = np.exp2(s.astype(float) - 127)
+    grid = np.concatenate([-R.GRID, R.GRID])
+    nearest = np.abs(x[..., None] / step[..., None] - grid).min(-1) * step
+    assert np.allclose(np.abs(x - v), nearest, rtol=0, atol=1e-12 * step.max()) or (np.abs(np.abs(x - v) - nearest) <= 1e-9 * step).all()
+    top = np.abs(x).max(-1, keepdims=True) / step
+    assert ((top > 3.5) | (s == 1)).all() and (top <= 7).all()
+
+
+def test_packed_bytes_and_pages_hold_what_was_put():
+    rs = np.random.default_rng(1)
+    c, s = R.quantize(rs.standard_normal((19, 544)))
+    p = R.pack(c, s)
+    assert len(p) == b.dllava_mx_bytes(19, 544) == 19 * 512 + 32 * 32
+    row, blk, el = 17, 16, 5
+    byte = p[row * 512 + (blk * 32 + el) // 2]
+    assert (byte >> 4) == c[row, blk * 32 + el]               # an odd element: the upper half
+    assert p[19 * 512 + (((row // 16 * 2 + blk // 16) * 4 + blk % 4) * 16 + row % 16) * 4 + blk % 16 // 4] == s[row, blk]
+    for Dh in (64, 128):
+        cache = R.Cache(np.full((6, 2, 17 * Dh), 0xFF, np.uint8), rs.permutation(6).reshape(2, 3), [0, 0])
+        kv = rs.standard_normal((2, 2, 40, 2, Dh))
+        for q in range(2):
+            for t in range(40):
+                cache.put(q, t, kv[q, 0, t], kv[q, 1, t])
+        for q in range(2):
+            K, V = cache.rows(q, 40)
+            assert np.array_equal(K, R.dequantize(*R.quantize(kv[q, 0]))) and np.array_equal(V, R.dequantize(*R.quantize(kv[q, 1])))
+
+
+# ---- refusals -----------------------------------------------------------------------------------------------------------------------
+FAKE = C.c_void_p(0x10000)       # never dereferenced: the calls below fail before anything is launched
+
+
+def _cache(dtype=2, Dh=64, page=16, H=2, pages=0x10000, mp=4):
+    return C.byref(b._KvCache(pages, 0x20000, 0x30000, 8, mp, page, H, Dh, dtype))
+
+
+CALLS = {
+    "dllava_mx_quantize": dict(x=FAKE, ldx=64, M=4, K=64, packed=FAKE, bytes=1 << 20, dtype=1),
+    "dllava_mx_dequantize": dict(packed=FAKE, bytes=1 << 20, M=4, K=64, y=FAKE, ldy=64, dtype=1),
+    "dllava_mx_linear": dict(xq=FAKE, xb=1 << 20, M=4, K=64, Wq=FAKE, wb=1 << 20, bias=None, N=16, act=0, residual=None, y=FAKE, ldy=16, dtype=1),
+    "dllava_mx_linear_few": dict(x=FAKE, ldx=64, M=4, K=64, Wq=FAKE, wb=1 << 20, bias=None, N=16, act=0, residual=None, y=FAKE, ldy=16, dtype=1),
+    "dllava_mx_cache_store": dict(K=FAKE, V=FAKE, ldkv=128, B=2, off=FAKE, start=None, rows=8, so=None, si=None, cache=_cache(), err=None, dtype=1),
+    "dllava_mx_cache_load": dict(cache=_cache(), B=2, off=FAKE, start=None, rows=8, K=FAKE, V=FAKE, ldkv=128, dtype=1),
+    "dllava_mx_decode_attn_append": dict(q=FAKE, k=FAKE, v=FAKE, B=2, Hq=4, logits=FAKE, threshold=0.0, ov=None, cache=_cache(), scale=0.1, o=FAKE,
+                                         ko=None, err=None, ws=FAKE, wb=1 << 30),
+    "dllava_group_prefill_attn": dict(Q=FAKE, ldq=256, K=FAKE, V=FAKE, ldkv=128, B=2, off=FAKE, rows=8, Hq=4, Hkv=2, Dh=64, scale=0.1, O=FAKE, dtype=1),
+}
+NAN = float("nan")
+ODD = C.c_void_p(0x10008)
+REFUSED = [
+    ("dllava_mx_quantize", EDTYPE, dict(dtype=2)), ("dllava_mx_quantize", EDTYPE, dict(dtype=-1)), ("dllava_mx_quantize", EINVAL, dict(M=-1)),
+    ("dllava_mx_quantize", EINVAL, dict(M=1 << 31)), ("dllava_mx_quantize", ESHAPE, dict(K=48)), ("dllava_mx_quantize", ESHAPE, dict(K=0)),
+    ("dllava_mx_quantize", EINVAL, dict(ldx=32)), ("dllava_mx_quantize", EINVAL, dict(ldx=68)), ("dllava_mx_quantize", ENULL, dict(x=None)),
+    ("dllava_mx_quantize", ENULL, dict(packed=None)), ("dllava_mx_quantize", EINVAL, dict(x=ODD)), ("dllava_mx_quantize", EINVAL, dict(packed=C.c_void_p(0x10080))),
+    ("dllava_mx_quantize", ECAPACITY, dict(bytes=1279)), ("dllava_mx_quantize", ESHAPE, dict(K=1 << 32)),
+    ("dllava_mx_dequantize", EDTYPE, dict(dtype=2)), ("dllava_mx_dequantize", ECAPACITY, dict(bytes=1279)), ("dllava_mx_dequantize", EINVAL, dict(ldy=60)),
+    ("dllava_mx_dequantize", ENULL, dict(y=None)), ("dllava_mx_dequantize", EINVAL, dict(y=ODD)),
+    ("dllava_mx_linear", EDTYPE, dict(dtype=0)), ("dllava_mx_linear", ESHAPE, dict(N=12)), ("dllava_mx_linear", ESHAPE, dict(N=-8)),
+    ("dllava_mx_linear", ESHAPE, dict(K=40)), ("dllava_mx_linear", ESHAPE, dict(K=1 << 23)), ("dllava_mx_linear", EINVAL, dict(act=3)),
+    ("dllava_mx_linear", EINVAL, dict(act=-1)), ("dllava_mx_linear", ENULL, dict(act=2)), ("dllava_mx_linear", EINVAL, dict(ldy=8)),
+    ("dllava_mx_linear", EINVAL, dict(ldy=20)), ("dllava_mx_linear", ENULL, dict(xq=None)), ("dllava_mx_linear", ENULL, dict(Wq=None)),
+    ("dllava_mx_linear", ENULL, dict(y=None)), ("dllava_mx_linear", ECAPACITY, dict(xb=1279)), ("dllava_mx_linear", ECAPACITY, dict(wb=4096)),
+    ("dllava_mx_linear", EINVAL, dict(xq=C.c_void_p(0x10010))), ("dllava_mx_linear", EINVAL, dict(Wq=C.c_void_p(0x10010))),
+    ("dllava_mx_linear", EINVAL, dict(bias=ODD)), ("dllava_mx_linear", EINVAL, dict(residual=ODD)), ("dllava_mx_linear", EINVAL, dict(y=ODD)),
+    ("dllava_mx_linear_few", ESHAPE, dict(M=65)), ("dllava_mx_linear_few", EINVAL, dict(M=-1)), ("dllava_mx_linear_few", EINVAL, dict(ldx=60)),
+    ("dllava_mx_linear_few", EINVAL, dict(ldx=68)), ("dllava_mx_linear_few", ENULL, dict(x=None)), ("dllava_mx_linear_few", EINVAL, dict(x=ODD)),
+    ("dllava_mx_linear_few", ECAPACITY, dict(wb=4096)), ("dllava_mx_linear_few", EDTYPE, dict(dtype=0)),
+    ("dllava_mx_cache_store", EDTYPE, dict(dtype=2)), ("dllava_mx_cache_store", EDTYPE, dict(cache=_cache(1))), ("dllava_mx_cache_store", ENULL, dict(cache=None)),
+    ("dllava_mx_cache_store", ESHAPE, dict(cache=_cache(Dh=96))), ("dllava_mx_cache_store", ESHAPE, dict(cache=_cache(page=32))),
+    ("dllava_mx_cache_store", EINVAL, dict(cache=_cache(pages=0x10008))), ("dllava_mx_cache_store", EINVAL, dict(ldkv=120)),
+    ("dllava_mx_cache_store", EINVAL, dict(ldkv=132)), ("dllava_mx_cache_store", ENULL, dict(off=None)), ("dllava_mx_cache_store", ENULL, dict(V=None)),
+    ("dllava_mx_cache_store", ENULL, dict(so=FAKE)), ("dllava_mx_cache_store", ENULL, dict(si=FAKE)), ("dllava_mx_cache_store", EINVAL, dict(B=-1)),
+    ("dllava_mx_cache_store", EINVAL, dict(rows=-1)), ("dllava_mx_cache_store", ESHAPE, dict(rows=1 << 31)),
+    ("dllava_mx_cache_store", EINVAL, dict(start=C.c_void_p(0x30000))), ("dllava_mx_cache_store", EINVAL, dict(start=C.c_void_p(0x30004))),
+    ("dllava_mx_cache_store", EINVAL, dict(start=C.c_void_p(0x2FFFC))), ("dllava_mx_cache_store", ESHAPE, dict(cache=_cache(mp=1 << 30))),
+    ("dllava_mx_cache_load", EDTYPE, dict(dtype=3)), ("dllava_mx_cache_load", EDTYPE, dict(cache=_cache(0))), ("dllava_mx_cache_load", ENULL, dict(K=None)),
+    ("dllava_mx_cache_load", EINVAL, dict(K=ODD)), ("dllava_mx_cache_load", EINVAL, dict(ldkv=64)),
+    ("dllava_mx_decode_attn_append", EDTYPE, dict(cache=_cache(1))), ("dllava_mx_decode_attn_append", ESHAPE, dict(Hq=5)),
+    ("dllava_mx_decode_attn_append", ESHAPE, dict(Hq=0)), ("dllava_mx_decode_attn_append", EINVAL, dict(threshold=NAN)),
+    ("dllava_mx_decode_attn_append", EINVAL, dict(scale=0.0)), ("dllava_mx_decode_attn_append", EINVAL, dict(scale=NAN)),
+    ("dllava_mx_decode_attn_append", EINVAL, dict(scale=float("inf"))), ("dllava_mx_decode_attn_append", ENULL, dict(logits=None)),
+    ("dllava_mx_decode_attn_append", ENULL, dict(o=None)), ("dllava_mx_decode_attn_append", EINVAL, dict(q=ODD)),
+    ("dllava_mx_decode_attn_append", EWORKSPACE, dict(wb=256)), ("dllava_mx_decode_attn_append", EWORKSPACE, dict(ws=None)),
+    ("dllava_mx_decode_attn_append", EWORKSPACE, dict(ws=ODD)), ("dllava_mx_decode_attn_append", EINVAL, dict(B=-1)),
+    ("dllava_mx_decode_attn_append", ESHAPE, dict(B=65536)),
+    ("dllava_group_prefill_attn", EDTYPE, dict(dtype=2)), ("dllava_group_prefill_attn", ESHAPE, dict(Dh=96)), ("dllava_group_prefill_attn", ESHAPE, dict(Hq=5)),
+    ("dllava_group_prefill_attn", ESHAPE, dict(Hkv=0)), ("dllava_group_prefill_attn", EINVAL, dict(ldq=192)), ("dllava_group_prefill_attn", EINVAL, dict(ldkv=132)),
+    ("dllava_group_prefill_attn", ESHAPE, dict(ldkv=(1 << 26) + 8)), ("dllava_group_prefill_attn", EINVAL, dict(scale=-1.0)),
+    ("dllava_group_prefill_attn", ENULL, dict(K=None)), ("dllava_group_prefill_attn", EINVAL, dict(V=ODD)), ("dllava_group_prefill_attn", ENULL, dict(off=None)),
+    ("dllava_group_prefill_attn", EINVAL, dict(rows=-1)), ("dllava_group_prefill_attn", ESHAPE, dict(rows=1 << 31)), ("dllava_group_prefill_attn", EINVAL, dict(B=-2)),
+]
+
+
+@pytest.mark.parametrize("name,status,change", REFUSED)
+def test_refused_on_the_host(name, status, change):
+    assert set(change) <= set(CALLS[name])
+    rc = getattr(b.lib(), name)(*{**CALLS[name], **change}.values(), None)
+    message = b.lib().dllava_last_error().decode()
+    assert rc == status and message, (rc, message)
+
+
+@pytest.mark.parametrize("name,change", [("dllava_mx_quantize", dict(M=0, x=None, packed=None, bytes=0)), ("dllava_mx_linear", dict(M=0, xq=None)),
+                                         ("dllava_mx_linear", dict(N=0, Wq=None, y=None)), ("dllava_mx_linear_few", dict(M=0, x=None)),
+                                         ("dllava_mx_cache_store", dict(B=0, off=None)), ("dllava_mx_cache_load", dict(rows=0, K=None, V=None)),
+                                         ("dllava_mx_decode_attn_append", dict(B=0, q=None)), ("dllava_group_prefill_attn", dict(rows=0, Q=None)),
+                                         ("dllava_group_prefill_attn", dict(B=0))])
+def test_nothing_to_do_is_no_error(name, change):
+    assert getattr(b.lib(), name)(*{**CALLS[name], **change}.values(), None) == 0
+
+
+def test_the_calls_of_dllava_h_refuse_a_cache_in_4_bits():
+    L = b.lib()
+    assert L.dllava_prefill_attn(FAKE, None, None, _cache(), 1, FAKE, 8, 2, 64, 0.1, FAKE, 1, None) == EDTYPE
+    assert L.dllava_decode_attn_append(FAKE, FAKE, FAKE, 2, FAKE, 0.0, None, _cache(), 0.1, FAKE, None, None, FAKE, 1 << 24, None) == EDTYPE
+    assert L.dllava_compact(2, FAKE, FAKE, FAKE, 8, None, None, 0, None, None, FAKE, FAKE, _cache(), None, 1, None) == EDTYPE
+
+
+def test_sizes():
+    assert b.dllava_mx_bytes(0, 64) == 0 and b.dllava_mx_bytes(4, 33) == 0 and b.dllava_mx_bytes(4, 0) == 0 and b.dllava_mx_bytes(-1, 64) == 0
+    assert b.dllava_mx_bytes(16, 512) == 16 * 256 + 256 and b.dllava_mx_bytes(1, 32) == 256 + 256 and b.dllava_mx_bytes(17, 544) == 17 * 512 + 32 * 32
+    for B, Hq, H in ((1, 32, 32), (1, 32, 8), (64, 32, 8), (32, 512, 32), (4096, 8, 8)):
+        n = b.dllava_mx_decode_workspace(B, Hq, H, 128, 100)
+        assert n % 256 == 0 and n >= 256 * B * (1 + H) and n < (64 << 20) + 256 * B * (1 + 2 * H)
+    assert b.dllava_mx_decode_workspace(0, 8, 8, 64, 1) == 256
+
+
+def test_exports_and_native_forms():
+    src = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "dllava_mx.h")).read(), flags=re.S)
+    assert set(b.EXPORTS_MX) == set(re.findall(r"\b(dllava_[a-z_]+)\s*\(", src))
+    import paper_2412_00876_amd as P
+    for n in b.EXPORTS_MX:
+        f = getattr(P, n)
+        if "stream" in inspect.signature(f).parameters:
+            assert type(f).__name__ == "Call" and inspect.isfunction(f.__wrapped__) and list(inspect.signature(f).parameters)[-1] == "stream"
+            assert n in CALLS
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="calls with host pointers: only where nothing can be launched")
+@pytest.mark.parametrize("name", sorted(CALLS))
+def test_native_and_python_forms_agree(name, monkeypatch):
+    from paper_2412_00876_amd import _calls
+    monkeypatch.setattr(b, "_stream", lambda stream: None)
+    _calls.init(b.KVCache, b.Predictor, b._check, lambda: 0, lambda: 0, lambda device: 0)
+    try:
+        cache = b.KVCache(torch.zeros(4, 2, 17 * 64, dtype=torch.uint8), torch.zeros(2, 2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32))
+        assert cache.c.dtype == b.MX and (cache.H, cache.Dh, cache.page_size) == (2, 64, 16)
+        t = torch.zeros(128, dtype=torch.uint8)
+        args = [cache if p == "cache" else dict(dtype=9, scale=0.1, threshold=NAN, M=4, K=64, N=16, act=0, B=2, rows=8, Hq=4, Hkv=2, Dh=64, ldx=64, ldy=64,
+                                                ldq=256, ldkv=128).get(p, t) if p != "K" or name.startswith(("dllava_mx_q", "dllava_mx_deq", "dllava_mx_lin")) else t
+                for p in inspect.signature(getattr(b, name)).parameters if p != "stream"]
+
+        def outcome(f, *a):
+            try:
+                return f(*a)
+            except Exception as e:  # noqa: BLE001
+                return type(e), getattr(e, "status", None), str(e)
+
+        f = getattr(b, name)
+        assert outcome(f, *args)[0] is b.DllavaError
+        for i in range(len(args)):
+            for v in (None, -3, 1 << 33, 1.5, "text", t, cache):
+                a = [*args[:i], v, *args[i + 1:]]
+                assert outcome(f, *a) == outcome(f.__wrapped__, *a), (i, v)
+    finally:
+        _calls.init(b.KVCache, b.Predictor, b._check, torch.cuda.current_device, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
