@@ -22,16 +22,10 @@ struct MxLinearArgs {
   int32_t act;         // 1: GELU; 2: times SiLU(R) instead of plus R
 };
 
-// One result per feature n .. n + 3 of row m, rounded once.
-__device__ __forceinline__ void mx_store_results(const MxLinearArgs& a, int64_t m, int n, float4 v) {
-  if (a.bias) {
-    const float4 b = *reinterpret_cast<const float4*>(a.bias + n);
-    v.x += b.x, v.y += b.y, v.z += b.z, v.w += b.w;
-  }
+// Four results, with the bias in them, to what is stored; r: the residual's or the gate's four values, where there are any.
+__device__ __forceinline__ uint2 mx_result(const MxLinearArgs& a, float4 v, const uint2& p) {
   if (a.act == 1) v = make_float4(gelu_erf_fast(v.x), gelu_erf_fast(v.y), gelu_erf_fast(v.z), gelu_erf_fast(v.w));
-  const int64_t at = m * a.ldy + n;
   if (a.R) {
-    const uint2 p = *reinterpret_cast<const uint2*>(a.R + at);
     const float r[4] = {bf16lo_to_f32(p.x), bf16hi_to_f32(p.x), bf16lo_to_f32(p.y), bf16hi_to_f32(p.y)};
     if (a.act == 2) {
       auto silu = [](float x) { return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896340736f * x)); };
@@ -40,7 +34,16 @@ __device__ __forceinline__ void mx_store_results(const MxLinearArgs& a, int64_t 
       v.x += r[0], v.y += r[1], v.z += r[2], v.w += r[3];
     }
   }
-  *reinterpret_cast<uint2*>(a.Y + at) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+  return make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
+}
+// The results of features n .. n + 3 of row m, each rounded once.
+__device__ __forceinline__ void mx_store_results(const MxLinearArgs& a, int64_t m, int n, float4 v) {
+  if (a.bias) {
+    const float4 b = *reinterpret_cast<const float4*>(a.bias + n);
+    v.x += b.x, v.y += b.y, v.z += b.z, v.w += b.w;
+  }
+  const int64_t at = m * a.ldy + n;
+  *reinterpret_cast<uint2*>(a.Y + at) = mx_result(a, v, a.R ? *reinterpret_cast<const uint2*>(a.R + at) : make_uint2(0u, 0u));
 }
 
 }  // namespace dllava
