@@ -129,6 +129,37 @@ def test_linear(M, K, N, act, bias, residual):
         assert torch.equal(r, y)
 
 
+@pytest.mark.parametrize("tile", [2, 4, 6, 7, 8, 12])
+@pytest.mark.parametrize("M,K,N,act,bias,residual", [(1, 32, 8, 0, True, False), (257, 512, 264, 0, False, False), (300, 544, 520, 2, True, True),
+                                                     (70, 2048, 1032, 1, True, True), (513, 1056, 776, 0, True, True), (130, 1536, 72, 1, False, False)])
+def test_every_tile(M, K, N, act, bias, residual, tile):
+    P.dllava_set_launch_override(7, tile)                   # DLLAVA_LAUNCH_LINEAR_TILE
+    try:
+        test_linear(M, K, N, act, bias, residual)
+    finally:
+        P.dllava_set_launch_override(7, 0)
+
+
+@pytest.mark.parametrize("tile,K", [(4, 96), (8, 512), (12, 512), (12, 544), (7, 1056), (6, 1600)])
+def test_several_tiles_to_a_block(tile, K):
+    """More tiles than the chip holds at once: what a block requests for its next tile, through rows of one, two and more stages."""
+    M, N = 5000, 4104 if tile == 12 else 5128
+    rs = np.random.default_rng(tile)
+    x, W = torch.from_numpy(rs.standard_normal((M, K)).astype(np.float32)).to(DEV), torch.from_numpy(rs.standard_normal((N, K)).astype(np.float32)).to(DEV)
+    xq, Wq = (torch.empty(P.dllava_mx_bytes(n, K), dtype=torch.uint8, device=DEV) for n in (M, N))
+    P.dllava_mx_quantize(x, K, M, K, xq, P.F32), P.dllava_mx_quantize(W, K, N, K, Wq, P.F32)
+    P.dllava_mx_dequantize(xq, M, K, x, K, P.F32), P.dllava_mx_dequantize(Wq, N, K, W, K, P.F32)
+    y = torch.full((M + 1, N), 5.0, dtype=torch.bfloat16, device=DEV)
+    P.dllava_set_launch_override(7, tile)
+    try:
+        P.dllava_mx_linear(xq, M, K, Wq, None, N, 0, None, y, N, P.BF16)
+    finally:
+        P.dllava_set_launch_override(7, 0)
+    want, mag = x.double() @ W.double().t().contiguous(), x.double().abs() @ W.double().abs().t().contiguous()
+    tol = 2.0 ** -8 * want.abs() + (K + 8) * 2.0 ** -23 * mag
+    assert ((y[:M].double() - want).abs() <= tol).all() and (y[M] == 5.0).all()
+
+
 @pytest.mark.parametrize("act,bias,residual", [(0, False, False), (0, True, True), (1, True, False), (2, False, True)])
 @pytest.mark.parametrize("M", [1, 2, 16, 17, 33, 49, 64])
 @pytest.mark.parametrize("K,N", [(32, 8), (96, 24), (1376, 520), (4096, 264), (11008, 40), (512, 8200), (96, 16400)])
