@@ -157,7 +157,7 @@ def test_sizes():
     assert b.dllava_mx_bytes(16, 512) == 16 * 256 + 256 and b.dllava_mx_bytes(1, 32) == 256 + 256 and b.dllava_mx_bytes(17, 544) == 17 * 512 + 32 * 32
     for B, Hq, H in ((1, 32, 32), (1, 32, 8), (64, 32, 8), (32, 512, 32), (4096, 8, 8)):
         n = b.dllava_mx_decode_workspace(B, Hq, H, 128, 100)
-        assert n % 256 == 0 and n >= 256 * B * (1 + H) and n < (64 << 20) + 256 * B * (1 + 2 * H)
+        assert n % 256 == 0 and 4096 < n < 16 << 20
     assert b.dllava_mx_decode_workspace(0, 8, 8, 64, 1) == 256
 
 
