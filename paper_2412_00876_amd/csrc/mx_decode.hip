@@ -265,6 +265,30 @@ __device__ __forceinline__ bool last_reader(const MxDecodeArgs& a, int ticket) {
   return true;
 }
 
+// Inclusive sum over the lanes up to this one, and the maximum of all (in lane 63), on the DPP data path.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int from_lane(int v, int otherwise) {
+  return __builtin_amdgcn_update_dpp(otherwise, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int scan_sum(int v) {
+  v += from_lane<0x111, 0xf>(v, 0);  // row_shr by 1, 2, 4, 8
+  v += from_lane<0x112, 0xf>(v, 0);
+  v += from_lane<0x114, 0xf>(v, 0);
+  v += from_lane<0x118, 0xf>(v, 0);
+  v += from_lane<0x142, 0xa>(v, 0);  // the last lane of rows 0 and 2 to the rows behind them
+  v += from_lane<0x143, 0xc>(v, 0);  // lane 31 to rows 2 and 3
+  return v;
+}
+__device__ __forceinline__ int scan_max(int v) {  // (of values >= 0)
+  int o;
+  o = from_lane<0x111, 0xf>(v, 0), v = o > v ? o : v;
+  o = from_lane<0x112, 0xf>(v, 0), v = o > v ? o : v;
+  o = from_lane<0x114, 0xf>(v, 0), v = o > v ? o : v;
+  o = from_lane<0x118, 0xf>(v, 0), v = o > v ? o : v;
+  o = from_lane<0x142, 0xa>(v, 0), v = o > v ? o : v;
+  o = from_lane<0x143, 0xc>(v, 0), v = o > v ? o : v;
+  return v;
+}
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 template <int DH>
@@ -290,15 +314,11 @@ __global__ __launch_bounds__(kThreads, 2) void mx_decode_kernel(MxDecodeArgs a) 
   int len_l = 0, total = 0, upto_l = 0, longest = 0;
   for (int b0 = 0; b0 < a.B; b0 += kWave) {
     len_l = b0 + lane < a.B ? read_len(b0 + lane) : 0;
-    upto_l = wave_incl_scan(b0 + lane < a.B ? steps_of(len_l) * HT : 0);
+    upto_l = scan_sum(b0 + lane < a.B ? steps_of(len_l) * HT : 0);
     total += __builtin_amdgcn_readlane(upto_l, kWave - 1);
     longest = len_l > longest ? len_l : longest;
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const int other = __shfl_xor(longest, o, kWave);
-    longest = other > longest ? other : longest;
-  }
+  longest = __builtin_amdgcn_readlane(scan_max(longest), kWave - 1);
   auto len_of = [&](int b) __attribute__((always_inline)) { return by_lane ? __builtin_amdgcn_readlane(len_l, b) : uniform(read_len(b)); };
   __syncthreads();
   int ticket = 0;
@@ -306,7 +326,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_decode_kernel(MxDecodeArgs a) 
   // The blocks' shares.  Equal ones, not too small, and so that a unit reaches into kBlocksPerUnit + 1 blocks at most; or, where that makes the
   // longest share kCut steps longer at most, each unit by itself in `parts` shares of its own (a cut costs two blocks a trip to memory and
   // one of them two more, about as long as kCut steps take a block).  Units are then numbered `pad` steps apart.
-  const int G = static_cast<int>(gridDim.x), even = (total + G - 1) / G, n_max = steps_of(uniform(longest)), units_all = a.B * HT;
+  const int G = static_cast<int>(gridDim.x), even = (total + G - 1) / G, n_max = steps_of(longest), units_all = a.B * HT;
   const int least = (n_max + kBlocksPerUnit - 1) / kBlocksPerUnit, parts = G / units_all < n_max / kLeastCut ? G / units_all : n_max / kLeastCut;
   const int alone = (n_max + (parts > 1 ? parts : 1) - 1) / (parts > 1 ? parts : 1);
   const bool apart = units_all <= G && alone <= even + kCut && alone >= least;
@@ -334,7 +354,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_decode_kernel(MxDecodeArgs a) 
       int len = len_l, upto = upto_l;
       if (!by_lane) {
         len = b0 + lane < a.B ? read_len(b0 + lane) : 0;
-        upto = wave_incl_scan(b0 + lane < a.B ? steps_of(len) * HT : 0);
+        upto = scan_sum(b0 + lane < a.B ? steps_of(len) * HT : 0);
       }
       const unsigned long long past = __ballot(below + upto > pos);
       if (past) {
@@ -361,9 +381,10 @@ __global__ __launch_bounds__(kThreads, 2) void mx_decode_kernel(MxDecodeArgs a) 
     p.b = uniform(p.b), p.h = uniform(p.h), p.tile = uniform(p.tile), p.s = uniform(p.s), p.n = uniform(p.n), p.L = uniform(p.L), p.start = uniform(p.start);
   };
 
+  Place here{0, 0, 0, 0, 1, 0, 0};
   if (apart && lo < hi) {  // of the unit's steps those that there are
-    const Place p = find(lo);
-    const int end = uniform(p.start + p.n);
+    here = find(lo);
+    const int end = uniform(here.start + here.n);
     if (hi > end) hi = end > lo ? end : lo;
   }
   const int wlo = uniform(lo + static_cast<int>(static_cast<int64_t>(hi - lo) * w / kWaves));
@@ -382,7 +403,9 @@ __global__ __launch_bounds__(kThreads, 2) void mx_decode_kernel(MxDecodeArgs a) 
   if (wlo < whi) {
     // The stream of loads: F is the next step to request, page[] its pages' numbers, scalar loads made one step before (the table does not change
     // while this kernel runs; as vector loads they would be waited for with everything that is in flight).
-    Place F = find(wlo);
+    if (apart) here.s += wlo - lo;
+    else here = find(wlo);
+    Place F = here;
     settle(F);
     Place C = F;                        // the step to work on
     int left = whi - wlo, to_load = left;
@@ -498,34 +521,13 @@ __global__ __launch_bounds__(kThreads, 2) void mx_decode_kernel(MxDecodeArgs a) 
   __syncthreads();
   if (!by_lane && tid == 0) ticket = reader_ticket(a);
 
-  // The waves' parts, in the order of their steps: those of one unit stand one behind the other.  Every part's factor, and the sums of the
-  // units (with the unit's first part) ...
+  // The waves' parts, in the order of their steps: those of one unit are joined, to its output or to a part of it -- the block's first unit and
+  // its last may reach into other blocks.
   constexpr int kParts = 2 * kWaves;
-  const int* const units = &sm_unit[0][0];
-  if (tid < kParts * kHeads) {
-    const int k = tid / kHeads, q = tid % kHeads, unit = units[k];
-    float M = -INFINITY, m[kParts];
-#pragma unroll
-    for (int j = 0; j < kParts; ++j) {
-      m[j] = units[j] == unit && unit >= 0 ? (&sm_m[0][0][0])[j * kHeads + q] : -INFINITY;
-      M = fmaxf(M, m[j]);
-    }
-    float l = 0.f;
-#pragma unroll
-    for (int j = 0; j < kParts; ++j) {
-      const float f = m[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[j] - M);
-      if (j == k) sm_f[tid] = f;
-      if (units[j] == unit) l += f * (&sm_l[0][0][0])[j * kHeads + q];
-    }
-    sm_f[kParts * kHeads + tid] = M;
-    sm_f[2 * kParts * kHeads + tid] = l;
-  }
-  __syncthreads();
-  // ... and their outputs, or their parts of them: the block's first unit and its last may reach into other blocks.
   int reach[2] = {-1, -1};
   // (Read by lanes, one each, and taken from there: as loads one behind the other they took longer than the sums.)
   const int in8 = lane % kParts;
-  const int unit_l = units[in8], start_l = (&sm_start[0][0])[in8], steps_l = (&sm_steps[0][0])[in8], q0_l = (&sm_q0[0][0])[in8], heads_l = (&sm_heads[0][0])[in8];
+  const int unit_l = (&sm_unit[0][0])[in8], start_l = (&sm_start[0][0])[in8], steps_l = (&sm_steps[0][0])[in8], q0_l = (&sm_q0[0][0])[in8], heads_l = (&sm_heads[0][0])[in8];
   bool known_l = unit_l < 0;
 #pragma unroll
   for (int j = 0; j < kParts - 1; ++j) known_l = known_l || (j < in8 && __builtin_amdgcn_readlane(unit_l, j) == unit_l);
@@ -545,15 +547,21 @@ __global__ __launch_bounds__(kThreads, 2) void mx_decode_kernel(MxDecodeArgs a) 
     float* const part = a.part + (static_cast<size_t>(blockIdx.x) * 2 + side) * a.part_heads * kPart;
     for (int i = tid; i < heads * (DH / 4); i += kThreads) {
       const int q = i / (DH / 4), c = i % (DH / 4) * 4;
+      float m[kParts], M = -INFINITY, l = 0.f;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int j = 0; j < kParts; ++j) {
+        m[j] = mine >> j & 1 ? (&sm_m[0][0][0])[j * kHeads + q] : -INFINITY;
+        M = fmaxf(M, m[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < kParts; ++j) {
         if (!(mine >> j & 1)) continue;
-        const float f = sm_f[j * kHeads + q];
+        const float f = m[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[j] - M);
         const float4 v = *reinterpret_cast<const float4*>(&sm_o[0][0][0][0] + (j * kHeads + q) * DH + c);
+        l += f * (&sm_l[0][0][0])[j * kHeads + q];
         o.x += f * v.x, o.y += f * v.y, o.z += f * v.z, o.w += f * v.w;
       }
-      const float l = sm_f[(2 * kParts + k) * kHeads + q];
       if (whole) {
         const float inv = 1.f / l;
         *reinterpret_cast<uint2*>(a.o + (q0 + q) * DH + c) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
@@ -563,7 +571,7 @@ __global__ __launch_bounds__(kThreads, 2) void mx_decode_kernel(MxDecodeArgs a) 
         st_agent(part + q * kPart + c + 2, o.z);
         st_agent(part + q * kPart + c + 3, o.w);
         if (c == 0) {
-          st_agent(part + q * kPart + DH, sm_f[(kParts + k) * kHeads + q]);
+          st_agent(part + q * kPart + DH, M);
           st_agent(part + q * kPart + DH + 1, l);
         }
       }
@@ -595,6 +603,32 @@ __global__ __launch_bounds__(kThreads, 2) void mx_decode_kernel(MxDecodeArgs a) 
         const int64_t block = first_block + j;
         return a.part + (static_cast<size_t>(block) * 2 + (start <= block * share ? 0 : 1)) * a.part_heads * kPart;
       };
+      constexpr int kFew = 6;
+      if (blocks <= kFew) {  // all on their way at once
+        for (int i = tid; i < heads * (DH / 2); i += kThreads) {
+          const int q = i / (DH / 2), c = i % (DH / 2) * 2;
+          float m[kFew], l[kFew], v[kFew][2], M = -INFINITY, sum = 0.f, x = 0.f, y = 0.f;
+#pragma unroll
+          for (int j = 0; j < kFew; ++j) {
+            const float* const p = part_of(j < blocks ? j : 0) + q * kPart;
+            m[j] = ld_agent(p + DH), l[j] = ld_agent(p + DH + 1), v[j][0] = ld_agent(p + c), v[j][1] = ld_agent(p + c + 1);
+          }
+#pragma unroll
+          for (int j = 0; j < kFew; ++j) {
+            if (j >= blocks) m[j] = -INFINITY;
+            M = fmaxf(M, m[j]);
+          }
+#pragma unroll
+          for (int j = 0; j < kFew; ++j) {
+            if (j >= blocks) continue;
+            const float f = m[j] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[j] - M);
+            sum += f * l[j], x += f * v[j][0], y += f * v[j][1];
+          }
+          const float inv = 1.f / sum;
+          *reinterpret_cast<uint32_t*>(a.o + (q0 + q) * DH + c) = pack_bf16x2(x * inv, y * inv);
+        }
+        continue;
+      }
       // the parts' references and sums, a thread each, then their factors
       float* const sm_w = &sm_o[0][0][0][0];  // (the waves' parts have been used)
       for (int i = tid; i < blocks * heads; i += kThreads) {
