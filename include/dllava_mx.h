@@ -65,7 +65,7 @@ int dllava_mx_linear(const void* xq, size_t xq_bytes, int64_t M, int64_t K, cons
 
 /*
  * The same for few rows (M <= 64: one per sequence of a decode step) that stay in bfloat16: only the weights are in 4 bits, and their
- * bytes are the traffic.  x [M, K] bfloat16, row stride ldx.  ldx % 8 == 0; otherwise as above.  No workspace.
+ * bytes are the traffic.  x [M, K] bfloat16, row stride ldx.  ldx % 8 == 0, ldx < 2^24; otherwise as above.  No workspace.
  */
 int dllava_mx_linear_few(const void* x, int64_t ldx, int64_t M, int64_t K, const void* Wq, size_t Wq_bytes, const float* bias, int64_t N,
                          int act, const void* residual, void* y, int64_t ldy, int dtype, void* stream);

@@ -1,11 +1,16 @@
 // dllava_mx_linear_few: y = act(x W^T + bias) (+ | *) residual for the few rows of a decode step, weights in 4 bits.
 //
-// The weights' 17/32 byte an element are the traffic.  A block of eight waves takes 16 * FT features and all rows; its waves
-// take windows of 512 columns in turn, add up their parts in registers and join them in LDS at the end, in the order of the
-// waves: no block waits for another, and no workspace is needed.  A lane reads 16 bytes of codes, 32 elements of one feature; they
-// become bfloat16 (exact: two significant bits times a power of two) in registers, four operands of v_mfma_f32_16x16x32_bf16, whose
-// columns are the rows of x.  The order in which a product runs over K is free: step s of a piece takes elements 8s .. 8s + 7 of each
-// lane's 32, and x is read to match.
+// The weights' 17/32 byte an element are the traffic from memory, but every block reads all of x: beside the 98 KB of weights that a compute
+// unit has of 4096 x 11008, 37 rows of x are 814 KB, from L2.  A block of eight waves takes 16 * FT features and all rows; its waves take
+// windows of 512 columns in turn, add up their parts in registers and join them in LDS at the end, in the order of the waves: no block
+// waits for another, and no workspace is needed.
+//  * x goes to LDS by asynchronous loads of whole 128-byte lines, tiles of 64 columns, a ring of D of them for each wave alone (no
+//    barriers).  (Straight to registers, in the layout of the products, the same bytes took twice as long: a load then touches parts of 32
+//    lines; 37 rows x 4096 features x 11008 columns 32 us instead of 19.3, but 1 x 4096 x 4096 5.0 instead of 5.4.)
+//  * A lane reads 16 bytes of codes, 32 elements of one feature, which become bfloat16 in registers (exact: two significant bits times a
+//    power of two), operands of v_mfma_f32_16x16x32_bf16, whose columns are the rows of x.  A product takes eight columns of each of its
+//    four lane groups, consecutive ones in LDS; the codes are exchanged between the groups to match, four swaps for 16 features x 128.
+#include "gemm_ring.h"
 #include "mx_linear.h"
 
 namespace dllava {
@@ -15,16 +20,50 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kWaves = 8;
+constexpr int kTileCols = 64;  // of x in LDS: a memory line of each row
 
-template <int FT>
-struct Weights {  // of one window: this lane's 32 elements of each of its four pieces, and their scales
-  uint4 c[FT][4];
-  uint32_t s[FT];
-};
+// A tile's operands from LDS: two of each 16 rows, 2 KB apart.  In asm since the compiler would wait for every asynchronous load first; the wait
+// is part of it, so that no register is taken as read before it is.
+template <int MT>
+__device__ __forceinline__ void lds_read_tile(ring_u32x4 (&x)[MT][2], uint32_t at0, uint32_t at1) {
+  if constexpr (MT == 1)
+    asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x[0][0]), "=&v"(x[0][1]) : "v"(at0), "v"(at1) : "memory");
+  if constexpr (MT == 2)
+    asm volatile(
+        "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %4 offset:2048\n\tds_read_b128 %3, %5 offset:2048\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1])
+        : "v"(at0), "v"(at1)
+        : "memory");
+  if constexpr (MT == 3)
+    asm volatile(
+        "ds_read_b128 %0, %6\n\tds_read_b128 %1, %7\n\tds_read_b128 %2, %6 offset:2048\n\tds_read_b128 %3, %7 offset:2048\n\t"
+        "ds_read_b128 %4, %6 offset:4096\n\tds_read_b128 %5, %7 offset:4096\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1])
+        : "v"(at0), "v"(at1)
+        : "memory");
+  if constexpr (MT == 4)
+    asm volatile(
+        "ds_read_b128 %0, %8\n\tds_read_b128 %1, %9\n\tds_read_b128 %2, %8 offset:2048\n\tds_read_b128 %3, %9 offset:2048\n\t"
+        "ds_read_b128 %4, %8 offset:4096\n\tds_read_b128 %5, %9 offset:4096\n\tds_read_b128 %6, %8 offset:6144\n\t"
+        "ds_read_b128 %7, %9 offset:6144\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1]), "=&v"(x[2][0]), "=&v"(x[2][1]), "=&v"(x[3][0]), "=&v"(x[3][1])
+        : "v"(at0), "v"(at1)
+        : "memory");
+}
 
-template <int FT, int MT>
+// FT tiles of 16 features, RG groups of eight rows (what a load of x covers).
+template <int FT, int RG>
 __global__ __launch_bounds__(kWaves* kWave) void mx_few_kernel(MxLinearArgs a) {
-  const int tid = threadIdx.x, lane = tid % kWave, w = tid / kWave, g = lane / 16, r16 = lane % 16;
+  constexpr int MT = (RG + 1) / 2;  // tiles of 16 rows (of an odd RG's last one the upper rows are whatever LDS holds: not used)
+  constexpr int D = MT <= 2 ? 4 : (MT == 3 ? 3 : 2);
+  constexpr bool kSlots = 8 % D == 0;  // a tile's slot follows from its number
+  constexpr int kTileBytes = MT * 16 * kTileCols * 2, kWaveBytes = D * kTileBytes;
+  constexpr int kSumBytes = kWaves * FT * MT * kWave * 16, kLds = kWaves * kWaveBytes > kSumBytes ? kWaves * kWaveBytes : kSumBytes;
+  __shared__ __align__(1024) char smem_raw[kLds];
+  DLLAVA_LDS char* smem = (DLLAVA_LDS char*)smem_raw;
+  const int tid = threadIdx.x, lane = tid % kWave, g = lane / 16, r16 = lane % 16;
+  const int w = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n0 = blockIdx.x * 16 * FT;
   const int64_t row_bytes = static_cast<int64_t>(a.windows) * (kMxWindow / 2);
   const uint8_t* wrow[FT];
@@ -34,66 +73,119 @@ __global__ __launch_bounds__(kWaves* kWave) void mx_few_kernel(MxLinearArgs a) {
     const int n = n0 + 16 * f + r16 < a.N ? n0 + 16 * f + r16 : a.N - 1;  // features past N are computed and dropped
     const int tile = n0 + 16 * f < a.N ? n0 / 16 + f : (a.N - 1) / 16;
     wrow[f] = a.Wc + n * row_bytes + 16 * g;
-    srow[f] = a.Ws + static_cast<int64_t>(tile) * a.windows * 256 + 4 * lane;
+    srow[f] = a.Ws + static_cast<int64_t>(tile) * a.windows * 256 + 4 * r16;
   }
-  const bf16_t* xrow[MT];
+  // x as a buffer: what is behind it -- rows past M, and by a lane's choice columns past K -- reads as zeros.  A load covers eight rows of a
+  // tile; chunk c (of 8 columns) of row r lies at place c ^ ((r / 2) % 8) of the row.
+  const uint32_t ldx = static_cast<uint32_t>(a.ldx) * 2;
+  const auto X = __builtin_amdgcn_make_buffer_rsrc(const_cast<bf16_t*>(a.X), 0, static_cast<uint32_t>(a.M - 1) * ldx + static_cast<uint32_t>(a.K) * 2, 0x00020000);
+  const int dma_row = lane >> 3;
+  uint32_t dma_at[RG];
+  int dma_col[2];  // of rows 0..7 and 8..15 of every 16
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int64_t m = 16 * t + r16 < a.M ? 16 * t + r16 : a.M - 1;
-    xrow[t] = a.X + m * a.ldx + 32 * g;
+  for (int i = 0; i < RG; ++i) {
+    const int row = 8 * i + dma_row, chunk = (lane & 7) ^ ((row >> 1) & 7);
+    dma_at[i] = row < a.M ? static_cast<uint32_t>(row) * ldx + 16 * chunk : 0x80000000u;
   }
-  auto load = [&](Weights<FT>& p, int win) {
 #pragma unroll
-    for (int f = 0; f < FT; ++f) {
+  for (int i = 0; i < 2; ++i) dma_col[i] = 8 * ((lane & 7) ^ (((8 * i + dma_row) >> 1) & 7));
+  const uint32_t ring = static_cast<uint32_t>(w) * kWaveBytes;
+  auto request_x = [&](int col, int slot) __attribute__((always_inline)) {  // columns col .. col + 63
+    const bool ragged = col + kTileCols > a.K;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) p.c[f][j] = *reinterpret_cast<const uint4*>(wrow[f] + static_cast<int64_t>(win) * 256 + 64 * j);
-      p.s[f] = *reinterpret_cast<const uint32_t*>(srow[f] + static_cast<int64_t>(win) * 256);
+    for (int i = 0; i < RG; ++i) {
+      const uint32_t at = ragged && col + dma_col[i % 2] >= a.K ? 0x80000000u : dma_at[i];
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(X, (DLLAVA_LDS void*)(smem + ring + slot * kTileBytes + i * 1024), 16, at, col < a.K ? 2 * col : 0, 0, 0);
     }
   };
+  const uint32_t frag = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(smem)) + ring + r16 * 128;
+  const uint32_t swizzle = (r16 >> 1) & 7;
+
   f32x4 acc[FT][MT];
 #pragma unroll
   for (int f = 0; f < FT; ++f)
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  Weights<FT> p, next;
-  if (w < a.windows) load(p, w);
+  // A window is four pieces of 128 columns, two tiles each; blocks begin at different pieces.  On their way: the codes of the next four
+  // pieces, D - 1 tiles of x.
+  const int turn = static_cast<int>(blockIdx.x);
+  auto col_of = [&](int win, int tile) __attribute__((always_inline)) { return win * kMxWindow + 128 * ((tile / 2 + turn) % 4) + kTileCols * (tile % 2); };
+  uint4 c[4][FT];
+  uint32_t sc[FT][4], sc_next[FT][4];  // [i]: a byte for block i of each piece
+  auto load_w = [&](int win, int j) __attribute__((always_inline)) {
+#pragma unroll
+    for (int f = 0; f < FT; ++f) c[j][f] = *reinterpret_cast<const uint4*>(wrow[f] + static_cast<int64_t>(win) * 256 + 64 * ((j + turn) % 4));
+  };
+  auto load_s = [&](int win) __attribute__((always_inline)) {
+#pragma unroll
+    for (int f = 0; f < FT; ++f)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sc_next[f][i] = *reinterpret_cast<const uint32_t*>(srow[f] + static_cast<int64_t>(win) * 256 + 64 * i);
+  };
+  if (w < a.windows) {
+    load_s(w);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) load_w(w, j);
+#pragma unroll
+    for (int t = 0; t < D - 1; ++t) request_x(col_of(w, t), t);
+  }
+  int slot_now = 0;  // of the tile at hand, where it does not follow from the tile's number
   for (int win = w; win < a.windows; win += kWaves) {
-    if (win + kWaves < a.windows) load(next, win + kWaves);
+    const int next = win + kWaves < a.windows ? win + kWaves : win;  // (past the end: this one again, not used)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int col = win * kMxWindow + 128 * j;
-      const bool in = col + 32 * g < a.K;  // behind K the weights' codes are zeros; x is not there
-      uint4 x[MT][4];
+    for (int f = 0; f < FT; ++f)
 #pragma unroll
-      for (int t = 0; t < MT; ++t)
+      for (int i = 0; i < 4; ++i) sc[f][i] = sc_next[f][i];
+    load_s(next);
+    uint32_t words[FT][4];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) x[t][s] = in ? *reinterpret_cast<const uint4*>(xrow[t] + col + 8 * s) : make_uint4(0, 0, 0, 0);
+    for (int tile = 0; tile < 8; ++tile) {
+      const int j = tile / 2, ahead = tile + D - 1, slot = kSlots ? tile % D : slot_now;
+      request_x(col_of(ahead < 8 ? win : next, ahead % 8), slot == 0 ? D - 1 : slot - 1);
+      if (tile % 2 == 0) {
 #pragma unroll
-      for (int f = 0; f < FT; ++f) {
-        const uint32_t sb = p.s[f] >> (8 * j) << 23;
-        const uint32_t c[4] = {p.c[f][j].x, p.c[f][j].y, p.c[f][j].z, p.c[f][j].w};
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          const bf16x8 wv = __builtin_bit_cast(bf16x8, mx_decode8(c[s], sb));
-#pragma unroll
-          for (int t = 0; t < MT; ++t) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, __builtin_bit_cast(bf16x8, x[t][s]), acc[f][t], 0, 0, 0);
+        for (int f = 0; f < FT; ++f) {
+          // word i of lane group g: columns 8i of block g -> word i: columns 8g of block i
+          const auto p02 = __builtin_amdgcn_permlane32_swap(c[j][f].x, c[j][f].z, false, false);
+          const auto p13 = __builtin_amdgcn_permlane32_swap(c[j][f].y, c[j][f].w, false, false);
+          const auto p01 = __builtin_amdgcn_permlane16_swap(p02[0], p13[0], false, false);
+          const auto p23 = __builtin_amdgcn_permlane16_swap(p02[1], p13[1], false, false);
+          words[f][0] = p01[0], words[f][1] = p01[1], words[f][2] = p23[0], words[f][3] = p23[1];
         }
       }
+      // this wave's loads of the tile have landed: RG loads of each of the D - 1 tiles behind it may be on their way (and whatever else was
+      // requested since, which only makes the wait longer)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 1) * RG) : "memory");
+      ring_u32x4 x[MT][2];
+      lds_read_tile<MT>(x, frag + slot * kTileBytes + (g ^ swizzle) * 16, frag + slot * kTileBytes + ((4 + g) ^ swizzle) * 16);
+#pragma unroll
+      for (int f = 0; f < FT; ++f) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t sb = sc[f][2 * (tile % 2) + i] >> (8 * ((j + turn) % 4)) << 23;
+          const bf16x8 wv = __builtin_bit_cast(bf16x8, mx_decode8(words[f][2 * (tile % 2) + i], sb));
+#pragma unroll
+          for (int t = 0; t < MT; ++t) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, __builtin_bit_cast(bf16x8, x[t][i]), acc[f][t], 0, 0, 0);
+        }
+      }
+      if (tile % 2 == 1) load_w(next, j);
+      if (!kSlots) slot_now = slot_now + 1 < D ? slot_now + 1 : 0;
     }
-    p = next;
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (tiles requested past the end)
+  __syncthreads();                                   // the rings' memory takes the sums
   // register e of acc[f][t]: feature n0 + 16 f + 4 g + e, row 16 t + r16
-  __shared__ float4 sm[kWaves][FT * MT][kWave];
+  float4* const sm = reinterpret_cast<float4*>(smem_raw);  // [kWaves][FT * MT][kWave]
 #pragma unroll
   for (int f = 0; f < FT; ++f)
 #pragma unroll
-    for (int t = 0; t < MT; ++t) sm[w][f * MT + t][lane] = make_float4(acc[f][t][0], acc[f][t][1], acc[f][t][2], acc[f][t][3]);
+    for (int t = 0; t < MT; ++t) sm[(w * FT * MT + f * MT + t) * kWave + lane] = make_float4(acc[f][t][0], acc[f][t][1], acc[f][t][2], acc[f][t][3]);
   __syncthreads();
   for (int i = w; i < FT * MT; i += kWaves) {
-    float4 v = sm[0][i][lane];
+    float4 v = sm[i * kWave + lane];
 #pragma unroll
     for (int k = 1; k < kWaves; ++k) {
-      const float4 u = sm[k][i][lane];
+      const float4 u = sm[(k * FT * MT + i) * kWave + lane];
       v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
     }
     const int n = n0 + 16 * (i / MT) + 4 * g;
@@ -102,16 +194,29 @@ __global__ __launch_bounds__(kWaves* kWave) void mx_few_kernel(MxLinearArgs a) {
   }
 }
 
-template <int FT>
-int launch_rows(const MxLinearArgs& a, hipStream_t st) {
-  const dim3 grid(static_cast<unsigned>(ceil_div(a.N, 16 * FT))), block(kWaves * kWave);
-  const int64_t tiles = ceil_div(a.M, 16);
-  if (tiles == 1) hipLaunchKernelGGL((mx_few_kernel<FT, 1>), grid, block, 0, st, a);
-  else if (tiles == 2) hipLaunchKernelGGL((mx_few_kernel<FT, 2>), grid, block, 0, st, a);
-  else if (tiles == 3) hipLaunchKernelGGL((mx_few_kernel<FT, 3>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((mx_few_kernel<FT, 4>), grid, block, 0, st, a);
+template <int FT, int RG>
+int launch_few(const MxLinearArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((mx_few_kernel<FT, RG>), dim3(static_cast<unsigned>(ceil_div(a.N, 16 * FT))), dim3(kWaves * kWave), 0, st, a);
   DLLAVA_CHECK_LAUNCH("mx_few_kernel");
   return DLLAVA_OK;
+}
+template <int RG>
+int launch_rows(const MxLinearArgs& a, int ft, hipStream_t st) {
+  if (ft == 1) return launch_few<1, RG>(a, st);
+  return ft == 2 ? launch_few<2, RG>(a, st) : launch_few<3, RG>(a, st);
+}
+
+// Tiles of features per block: whole rounds of a block on each compute unit, each round 3 us, and for every 512 columns of a wave 0.6 us for eight
+// rows and 1.9 for 16 features.  Measured, one tile / two / three, in us: 1 row x 11008 features x 4096 columns 12.1 / 13.1 / 10.8, 64 rows 26.2 /
+// 23.8 / 16.6; 1 x 5120 x 13824 17.0 / 17.7 / 21.3, 64 52.5 / 33.7 / 41.0; 1 x 4096 x 4096 5.4 / 7.0 / 8.9; 37 x 4096 x 11008 19.3 / 23.6 / 28.7.
+int pick_features(const MxLinearArgs& a, int rg) {
+  int best = 1;
+  int64_t best_cost = 0;
+  for (int ft = 1; ft <= 3; ++ft) {
+    const int64_t rounds = ceil_div(ceil_div(a.N, 16 * ft), 256), cost = rounds * (24000 + a.windows * (600 * rg + 1900 * ft));
+    if (ft == 1 || cost < best_cost) best = ft, best_cost = cost;
+  }
+  return best;
 }
 
 }  // namespace
@@ -154,12 +259,24 @@ extern "C" int dllava_mx_linear_few(const void* x, int64_t ldx, int64_t M, int64
   if (int rc = mx_linear_check("mx_linear_few", M, K, Wq, Wq_bytes, bias, N, act, residual, y, ldy, dtype)) return rc;
   DLLAVA_REQUIRE(M <= 64, DLLAVA_ESHAPE, "mx_linear_few: at most 64 rows (got %lld); dllava_mx_linear takes more", (long long)M);
   DLLAVA_REQUIRE(ldx >= K && ldx % 8 == 0, DLLAVA_EINVAL, "mx_linear_few: ldx = %lld must be at least K and a multiple of 8", (long long)ldx);
+  // (64 rows of x are addressed by 31-bit offsets)
+  DLLAVA_REQUIRE(ldx < (int64_t{1} << 24), DLLAVA_ESHAPE, "mx_linear_few: ldx = %lld must be below 2^24", (long long)ldx);
   if (M == 0 || N == 0) return DLLAVA_OK;
   DLLAVA_REQUIRE(x, DLLAVA_ENULL, "mx_linear_few: x is required");
   DLLAVA_REQUIRE(aligned(x, 16), DLLAVA_EINVAL, "mx_linear_few: x must be 16-byte aligned");
   MxLinearArgs a = mx_linear_args(M, K, Wq, bias, N, act, residual, y, ldy);
   a.X = static_cast<const bf16_t*>(x), a.ldx = ldx;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (N <= 16 * 512) return launch_rows<1>(a, st);
-  return launch_rows<2>(a, st);
+  const int rg = static_cast<int>(ceil_div(M, 8)), forced = launch_override(DLLAVA_LAUNCH_LINEAR_TILE);
+  const int ft = forced >= 1 && forced <= 3 ? forced : pick_features(a, rg);
+  switch (rg) {
+    case 1: return launch_rows<1>(a, ft, st);
+    case 2: return launch_rows<2>(a, ft, st);
+    case 3: return launch_rows<3>(a, ft, st);
+    case 4: return launch_rows<4>(a, ft, st);
+    case 5: return launch_rows<5>(a, ft, st);
+    case 6: return launch_rows<6>(a, ft, st);
+    case 7: return launch_rows<7>(a, ft, st);
+    default: return launch_rows<8>(a, ft, st);
+  }
 }

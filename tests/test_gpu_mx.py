@@ -181,6 +181,23 @@ def test_linear_few(M, K, N, act, bias, residual):
         assert torch.equal(r, y)
 
 
+@pytest.mark.parametrize("tiles", [1, 2, 3])
+@pytest.mark.parametrize("M", [3, 9, 23, 32, 37, 41, 56, 60])
+@pytest.mark.parametrize("K,N", [(64, 56), (1376, 104), (4640, 136)])
+def test_linear_few_with_each_tile(M, K, N, tiles):
+    rs = np.random.default_rng(M + K + N + tiles)
+    x = rows_of(rs, M, K, torch.bfloat16, K + 8)
+    Wq, W = packed(rs, N, K, K ** -0.5)
+    y = torch.full((M + 1, N), 5.0, dtype=torch.bfloat16, device=DEV)
+    P.dllava_set_launch_override(7, tiles)
+    try:
+        P.dllava_mx_linear_few(x, K + 8, M, K, Wq, None, N, 0, None, y, N, P.BF16)
+    finally:
+        P.dllava_set_launch_override(7, 0)
+    check_linear(y[:M], f64(x[:, :K]), W, None, 0, None, K)
+    assert (y[M] == 5.0).all()
+
+
 def test_nan_stays_in_its_row():
     """A block with an infinity makes its row NaN, in the rows' and in the weights' part, and no other."""
     rs = np.random.default_rng(3)

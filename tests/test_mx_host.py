@@ -100,7 +100,7 @@ REFUSED = [
     ("dllava_mx_linear", EINVAL, dict(xq=C.c_void_p(0x10010))), ("dllava_mx_linear", EINVAL, dict(Wq=C.c_void_p(0x10010))),
     ("dllava_mx_linear", EINVAL, dict(bias=ODD)), ("dllava_mx_linear", EINVAL, dict(residual=ODD)), ("dllava_mx_linear", EINVAL, dict(y=ODD)),
     ("dllava_mx_linear_few", ESHAPE, dict(M=65)), ("dllava_mx_linear_few", EINVAL, dict(M=-1)), ("dllava_mx_linear_few", EINVAL, dict(ldx=60)),
-    ("dllava_mx_linear_few", EINVAL, dict(ldx=68)), ("dllava_mx_linear_few", ENULL, dict(x=None)), ("dllava_mx_linear_few", EINVAL, dict(x=ODD)),
+    ("dllava_mx_linear_few", EINVAL, dict(ldx=68)), ("dllava_mx_linear_few", ESHAPE, dict(ldx=1 << 24)), ("dllava_mx_linear_few", ENULL, dict(x=None)), ("dllava_mx_linear_few", EINVAL, dict(x=ODD)),
     ("dllava_mx_linear_few", ECAPACITY, dict(wb=4096)), ("dllava_mx_linear_few", EDTYPE, dict(dtype=0)),
     ("dllava_mx_cache_store", EDTYPE, dict(dtype=2)), ("dllava_mx_cache_store", EDTYPE, dict(cache=_cache(1))), ("dllava_mx_cache_store", ENULL, dict(cache=None)),
     ("dllava_mx_cache_store", ESHAPE, dict(cache=_cache(Dh=96))), ("dllava_mx_cache_store", ESHAPE, dict(cache=_cache(page=32))),
@@ -200,3 +200,22 @@ def test_native_and_python_forms_agree(name, monkeypatch):
                 assert outcome(f, *a) == outcome(f.__wrapped__, *a), (i, v)
     finally:
         _calls.init(b.KVCache, b.Predictor, b._check, torch.cuda.current_device, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
+
+
+def test_kernels_do_not_spill():
+    """The loops over weights, rows and pages count their loads in flight: scratch traffic would add to that count."""
+    import subprocess
+    from concurrent.futures import ThreadPoolExecutor
+    from paper_2412_00876_amd import build
+
+    def report(source):
+        r = subprocess.run([build.HIPCC, *build.COMMON, *build.HIP_FLAGS, "-Rpass-analysis=kernel-resource-usage", "--cuda-device-only", "-c",
+                            os.path.join(build.CSRC, source), "-o", os.devnull], capture_output=True, text=True)
+        assert r.returncode == 0, r.stderr[-2000:]
+        return r.stderr.split("Function Name: ")[1:]
+
+    with ThreadPoolExecutor(4) as ex:
+        for kernels in ex.map(report, ("mx_linear.hip", "mx_few.hip", "mx_decode.hip", "mx_quantize.hip", "mx_cache.hip", "group_prefill.hip")):
+            assert kernels
+            for b in kernels:
+                assert re.search(r"ScratchSize \[bytes/lane\]: 0\b", b), b[:400]
