@@ -45,7 +45,7 @@ size_t dllava_mx_bytes(int64_t M, int64_t K);   /* host, pure; 0 if a size is no
 
 /*
  * Rows to 4 bits.  x [M, K] dtype (DLLAVA_F32 or DLLAVA_BF16), row stride ldx; packed: out, fully written.
- * Sizes: K % 32 == 0, ldx * sizeof(dtype) % 16 == 0, ldx >= K, M < 2^31.  M == 0 is a no-op.
+ * Sizes: K % 32 == 0, ldx * sizeof(dtype) % 16 == 0, ldx >= K, ceil(M / 16) * ceil(K / 512) < 2^24.  M == 0 is a no-op.
  */
 int dllava_mx_quantize(const void* x, int64_t ldx, int64_t M, int64_t K, void* packed, size_t packed_bytes, int dtype, void* stream);
 
@@ -58,7 +58,7 @@ int dllava_mx_dequantize(const void* packed, size_t packed_bytes, int64_t M, int
  *   xq  packed [M, K];  Wq  packed [N, K];  bias [N] float32 or NULL;
  *   residual [M, N] bfloat16 with y's row stride, or NULL (act 0, 1), may be y itself;  y [M, N] bfloat16, row stride ldy, out.
  * Products are exact, sums are float32, each result is rounded once.
- * Sizes: K % 32 == 0, N % 8 == 0, ldy % 8 == 0, K < 2^23.  dtype: DLLAVA_BF16.  M == 0 or N == 0 is a no-op.
+ * Sizes: K % 32 == 0, N % 8 == 0, ldy % 8 == 0, K < 2^23, N < 2^27.  dtype: DLLAVA_BF16.  M == 0 or N == 0 is a no-op.
  */
 int dllava_mx_linear(const void* xq, size_t xq_bytes, int64_t M, int64_t K, const void* Wq, size_t Wq_bytes, const float* bias, int64_t N,
                      int act, const void* residual, void* y, int64_t ldy, int dtype, void* stream);
@@ -80,7 +80,7 @@ int dllava_mx_linear_few(const void* x, int64_t ldx, int64_t M, int64_t K, const
  *            dllava_select_compact): it is row src_off[b] + src_idx[off[b] + i], so that only the kept rows are stored
  *   err_flag device int32, may be NULL: set to 1 if some sequence exceeds max_pages_per_seq * page_size; rows beyond it are
  *            not stored and cache_len[b] is clamped to it.  Never cleared by the library.
- * Only the slots of the stored tokens are written.  Positions before start[b] keep what they hold.
+ * Only the slots of the stored tokens are written.  Positions before start[b] keep what they hold.  Sizes: rows / 16 + 2 B < 2^24.
  */
 int dllava_mx_cache_store(const void* K, const void* V, int64_t ldkv, int32_t B, const int32_t* off, const int32_t* start, int64_t rows,
                           const int32_t* src_off, const int32_t* src_idx, const dllava_kv_cache* cache, int32_t* err_flag, int dtype,

@@ -2,8 +2,10 @@
 //
 // Pure streams.  A wave takes one head of one page's piece of a sequence: 16 tokens at most, a lane eight elements of a token (four
 // lanes a block of 32).  Keys keep their order.  A byte of the values holds columns c and c + 16 of a block, which lie in lanes two
-// apart: the two exchange their codes and write half of the bytes each.  No byte is shared between tokens, so tokens of other calls in the
-// same page are left alone.
+// apart, and the bytes of a token's blocks at equal columns lie together: the lanes exchange their codes (two apart, then the blocks'
+// lanes, four and eight apart) and each writes a word of whole bytes.  No byte is shared between tokens, so tokens of other calls in the same page
+// are left alone.  Measured, 16 sequences of 352 of 704 rows, 32 heads of 128, bfloat16 (117 MB, 24 us at the rate of a copy): 29.6 us in,
+// 30.4 us out; 36.1 and 41.3 with the values' bytes one by one.
 #include "mx.h"
 
 namespace dllava {
@@ -51,10 +53,12 @@ struct Piece {
 // Pieces are numbered in slots: those of sequence b from off[b] / 16 + 2b on (a sequence of n rows touches at most n / 16 + 2 pages).
 // n == 0: none.
 __device__ __forceinline__ Piece find_piece(const CacheArgs& a, int slot) {
-  int lo = 0, hi = a.B;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (a.off[mid] / kPage + 2 * mid <= slot) lo = mid; else hi = mid;
+  int lo = 0;
+  for (int n = a.B; n > 1;) {  // 64 sequences in question at a time
+    const int step = (n + kWave - 1) / kWave, i = static_cast<int>(threadIdx.x % kWave) * step, mid = lo + i;
+    const uint64_t at = __ballot(i < n && a.off[i < n ? mid : lo] / kPage + 2 * (i < n ? mid : lo) <= slot);
+    const int last = at ? 63 - __clzll(at) : 0;
+    lo += last * step, n = n - last * step < step ? n - last * step : step;
   }
   Piece p{lo, 0, 0, 0, false};
   const int r0 = a.off[lo], end = a.off[lo + 1] < a.rows ? a.off[lo + 1] : a.rows, i = slot - (r0 / kPage + 2 * lo);
@@ -71,6 +75,53 @@ __device__ __forceinline__ uint8_t* head_of(const CacheArgs& a, const Piece& p, 
   return a.pages + (static_cast<size_t>(page) * a.H + h) * mx_page_bytes(DH);
 }
 
+template <int CTRL>
+__device__ __forceinline__ uint32_t lanes(uint32_t v) {
+  return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true);
+}
+__device__ __forceinline__ uint32_t lane_xor2(uint32_t v) { return lanes<0x4E>(v); }                // quad_perm [2,3,0,1]
+__device__ __forceinline__ uint32_t lane_xor4(uint32_t v) { return lanes<0x141>(lanes<0x1B>(v)); }  // quad_perm [3,2,1,0], row_half_mirror
+__device__ __forceinline__ uint32_t lane_xor8(uint32_t v) { return lanes<0x128>(v); }               // row_ror:8
+// Byte e of lane m's word to byte m of lane e's, m the lane's block: of four (Dh = 128, lanes 4 apart), or of two (the words' halves: bytes
+// 0 and 1 of lane e hold what both have in byte e, bytes 2 and 3 what they have in byte e + 2).  Twice is once undone.
+template <int BLOCKS>
+__device__ __forceinline__ uint32_t transpose_blocks(uint32_t w, int m) {
+  const uint32_t o = lane_xor4(w);
+  w = __builtin_amdgcn_perm(o, w, m & 1 ? 0x03070105u : 0x06020400u);  // bytes 0..3: w's, 4..7: o's
+  if (BLOCKS == 4) {
+    const uint32_t far = lane_xor8(w);
+    w = __builtin_amdgcn_perm(far, w, m & 2 ? 0x03020706u : 0x05040100u);
+  }
+  return w;
+}
+__device__ __forceinline__ uint32_t nibbles_to_bytes(uint32_t x) {  // of the lower half
+  x = (x | x << 8) & 0x00ff00ffu;
+  return (x | x << 4) & 0x0f0f0f0fu;
+}
+__device__ __forceinline__ uint32_t bytes_to_nibbles(uint32_t x) {  // their lower four bits
+  x &= 0x0f0f0f0fu;
+  x = (x | x >> 4) & 0x00ff00ffu;
+  return (x | x >> 8) & 0xffffu;
+}
+// A lane's words of a token's values: bytes of all blocks at column c0 + m (and, of two blocks, at c0 + m + 2 in the upper half).
+template <int DH>
+struct ValueBytes {
+  static constexpr int kBlocks = DH / kMxBlock;
+  static __device__ __forceinline__ int at(int t, int c) { return 8 * DH + ((t / 4 * 16 + c) * 4 + t % 4) * kBlocks; }
+  static __device__ __forceinline__ void store(uint8_t* page, int t, int c0, int m, uint32_t w) {
+    if constexpr (kBlocks == 4) {
+      *reinterpret_cast<uint32_t*>(page + at(t, c0 + m)) = w;
+    } else {
+      *reinterpret_cast<uint16_t*>(page + at(t, c0 + m)) = static_cast<uint16_t>(w);
+      *reinterpret_cast<uint16_t*>(page + at(t, c0 + m + 2)) = static_cast<uint16_t>(w >> 16);
+    }
+  }
+  static __device__ __forceinline__ uint32_t load(const uint8_t* page, int t, int c0, int m) {
+    if constexpr (kBlocks == 4) return *reinterpret_cast<const uint32_t*>(page + at(t, c0 + m));
+    return *reinterpret_cast<const uint16_t*>(page + at(t, c0 + m)) | static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(page + at(t, c0 + m + 2))) << 16;
+  }
+};
+
 template <typename T, int DH>
 __global__ __launch_bounds__(kThreads) void mx_cache_store_kernel(CacheArgs a) {
   constexpr int kLanes = DH / 8, kTokens = kWave / kLanes, kSteps = kPage / kTokens, kBlocks = DH / kMxBlock;
@@ -84,44 +135,35 @@ __global__ __launch_bounds__(kThreads) void mx_cache_store_kernel(CacheArgs a) {
   const Piece p = find_piece(a, blockIdx.x);
   const int lane = threadIdx.x % kWave, h = blockIdx.y * kWaves + threadIdx.x / kWave;
   if (p.n == 0 || !p.inside || h >= a.H) return;
-  const int i8 = lane % kLanes, t_in = lane / kLanes;
+  const int i8 = lane % kLanes, t_in = lane / kLanes, m = i8 / 4;
   uint8_t* const page = head_of(a, p, h, DH);
   const int32_t r0 = a.off[p.b];
   float k[kSteps][8], v[kSteps][8];
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
-    const int i = s * kTokens + t_in;
-    if (i < p.n) {
-      const int row = r0 + p.row + i;
-      const int64_t src = (a.src_idx ? static_cast<int64_t>(a.src_off[p.b]) + a.src_idx[row] : row) * a.ldkv + static_cast<int64_t>(h) * DH + 8 * i8;
-      mx_load8(static_cast<const T*>(a.K) + src, k[s]);
-      mx_load8(static_cast<const T*>(a.V) + src, v[s]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) k[s][e] = v[s][e] = 0.f;
-    }
+    const int i = s * kTokens + t_in, row = r0 + p.row + (i < p.n ? i : 0);  // (past the piece: its first token, not stored)
+    const int64_t src = (a.src_idx ? static_cast<int64_t>(a.src_off[p.b]) + a.src_idx[row] : row) * a.ldkv + static_cast<int64_t>(h) * DH + 8 * i8;
+    mx_load8(static_cast<const T*>(a.K) + src, k[s]);
+    mx_load8(static_cast<const T*>(a.V) + src, v[s]);
   }
+  // lane i8: block m, columns 8 (i8 % 4) ..: with the lane two apart, the lower half of the block's bytes where i8 % 4 < 2
+  const bool low = (i8 & 2) == 0;
+  const int c0 = 8 * (i8 & 1) + (low ? 0 : 4);
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
     const int i = s * kTokens + t_in, t = static_cast<int>(p.pos % kPage) + i;  // slot in the page
     const uint32_t ks = mx_scale_byte(mx_block_amax(k[s])), vs = mx_scale_byte(mx_block_amax(v[s]));
-    const uint32_t kc = mx_encode8(k[s], ks), mine = mx_encode8(v[s], vs);
-    const uint32_t other = __shfl_xor(mine, 2, kWave);
+    const uint32_t kc = mx_encode8(k[s], ks), mine = mx_encode8(v[s], vs), other = lane_xor2(mine);
+    const uint32_t lower = low ? mine & 0xffffu : other >> 16, upper = low ? other & 0xffffu : mine >> 16;
+    const uint32_t bytes = transpose_blocks<kBlocks>(nibbles_to_bytes(lower) | nibbles_to_bytes(upper) << 4, m);
+    const uint32_t scales = transpose_blocks<kBlocks>(ks | vs << 8, m);  // lane m = 0: of the keys' blocks, 1: of the values'
     if (i >= p.n) continue;
     *reinterpret_cast<uint32_t*>(page + t * (DH / 2) + 4 * i8) = kc;
-    // lane i8: block i8 / 4, columns 8 (i8 % 4) ..: the lower half of the block's bytes where i8 % 4 < 2
-    const bool low = (i8 & 2) == 0;
-    const uint32_t lo = low ? mine : other, hi = low ? other : mine;
-    const int c0 = 8 * (i8 & 1) + (low ? 0 : 4);
-    uint8_t* const dst = page + 8 * DH + ((t / 4 * 16 + c0) * 4 + t % 4) * kBlocks + i8 / 4;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int sh = 4 * e + (low ? 0 : 16);
-      dst[e * 4 * kBlocks] = static_cast<uint8_t>(((lo >> sh) & 15u) | (((hi >> sh) & 15u) << 4));
-    }
-    if (i8 % 4 == 0) {
-      page[16 * DH + t * kBlocks + i8 / 4] = static_cast<uint8_t>(ks);
-      page[16 * DH + DH / 2 + t * kBlocks + i8 / 4] = static_cast<uint8_t>(vs);
+    ValueBytes<DH>::store(page, t, c0, m, bytes);
+    if (i8 == 0 || i8 == 4) {
+      uint8_t* const dst = page + 16 * DH + m * (DH / 2) + t * kBlocks;
+      if constexpr (kBlocks == 4) *reinterpret_cast<uint32_t*>(dst) = scales;
+      else *reinterpret_cast<uint16_t*>(dst) = static_cast<uint16_t>(scales);
     }
   }
 }
@@ -132,25 +174,31 @@ __global__ __launch_bounds__(kThreads) void mx_cache_load_kernel(CacheArgs a) {
   const Piece p = find_piece(a, blockIdx.x);
   const int lane = threadIdx.x % kWave, h = blockIdx.y * kWaves + threadIdx.x / kWave;
   if (p.n == 0 || h >= a.H) return;
-  const int i8 = lane % kLanes, t_in = lane / kLanes;
-  const uint8_t* const page = p.inside ? head_of(a, p, h, DH) : nullptr;  // (positions behind the capacity have no page)
+  const int i8 = lane % kLanes, t_in = lane / kLanes, m = i8 / 4;
+  const uint8_t* const page = p.inside ? head_of(a, p, h, DH) : a.pages;  // (positions behind the capacity have no page; not used)
   const int len = p.inside ? a.cache_len[p.b] : 0;
+  const bool low = (i8 & 2) == 0;
+  const int c0 = 8 * (i8 & 1) + (low ? 0 : 4);
+  uint32_t kc[kSteps], w[kSteps], ks[kSteps], vs[kSteps];
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) {
-    const int i = s * kTokens + t_in, t = static_cast<int>(p.pos % kPage) + i;
-    if (i >= p.n) continue;
-    uint4 k = make_uint4(0, 0, 0, 0), v = k;
-    if (p.pos + i < len) {
-      k = mx_decode8(*reinterpret_cast<const uint32_t*>(page + t * (DH / 2) + 4 * i8), static_cast<uint32_t>(page[16 * DH + t * kBlocks + i8 / 4]) << 23);
-      const uint8_t* src = page + 8 * DH + ((t / 4 * 16 + 8 * (i8 & 1)) * 4 + t % 4) * kBlocks + i8 / 4;
-      uint32_t c = 0;
+    const int t = (static_cast<int>(p.pos % kPage) + s * kTokens + t_in) % kPage;  // (past the piece: another slot, not used)
+    kc[s] = *reinterpret_cast<const uint32_t*>(page + t * (DH / 2) + 4 * i8);
+    w[s] = ValueBytes<DH>::load(page, t, c0, m);
+    ks[s] = page[16 * DH + t * kBlocks + m], vs[s] = page[16 * DH + DH / 2 + t * kBlocks + m];
+  }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) c |= ((src[e * 4 * kBlocks] >> ((i8 & 2) ? 4 : 0)) & 15u) << (4 * e);
-      v = mx_decode8(c, static_cast<uint32_t>(page[16 * DH + DH / 2 + t * kBlocks + i8 / 4]) << 23);
-    }
+  for (int s = 0; s < kSteps; ++s) {
+    const int i = s * kTokens + t_in;
+    const uint32_t mine = transpose_blocks<kBlocks>(w[s], m);       // block m's bytes at columns c0 .. c0 + 3
+    const uint32_t other = lane_xor2(mine);                         // at the other four of 8 (i8 % 2) ..
+    const uint32_t codes = low ? bytes_to_nibbles(mine) | bytes_to_nibbles(other) << 16 : bytes_to_nibbles(other >> 4) | bytes_to_nibbles(mine >> 4) << 16;
+    if (i >= p.n) continue;
+    const bool held = p.pos + i < len;
+    const uint4 zero = make_uint4(0, 0, 0, 0);
     const int64_t dst = (static_cast<int64_t>(a.off[p.b]) + p.row + i) * a.ldkv + static_cast<int64_t>(h) * DH + 8 * i8;
-    mx_store8(const_cast<T*>(static_cast<const T*>(a.K)) + dst, k);
-    mx_store8(const_cast<T*>(static_cast<const T*>(a.V)) + dst, v);
+    mx_store8(const_cast<T*>(static_cast<const T*>(a.K)) + dst, held ? mx_decode8(kc[s], ks[s] << 23) : zero);
+    mx_store8(const_cast<T*>(static_cast<const T*>(a.V)) + dst, held ? mx_decode8(codes, vs[s] << 23) : zero);
   }
 }
 int prepare(const char* who, const void* K, const void* V, int64_t ldkv, int32_t B, const int32_t* off, const int32_t* start, int64_t rows,
@@ -162,7 +210,7 @@ int prepare(const char* who, const void* K, const void* V, int64_t ldkv, int32_t
                  "%s: ldkv = %lld must be at least H * Dh and a multiple of 16 bytes", who, (long long)ldkv);
   if (B == 0) return DLLAVA_OK;
   const int64_t pieces = rows / kPage + 2 * static_cast<int64_t>(B) + 1;
-  DLLAVA_REQUIRE(rows <= 0x7fffffffLL && pieces <= 0x7fffffffLL, DLLAVA_ESHAPE, "%s: rows and B must fit in int32", who);
+  DLLAVA_REQUIRE(rows <= 0x7fffffffLL && pieces < (1 << 24), DLLAVA_ESHAPE, "%s: rows / 16 + 2 B must be below 2^24", who);
   DLLAVA_REQUIRE(off && (rows == 0 || (K && V)), DLLAVA_ENULL, "%s: off, K and V are required", who);
   DLLAVA_REQUIRE(aligned(K, 16) && aligned(V, 16), DLLAVA_EINVAL, "%s: K and V must be 16-byte aligned", who);
   a.K = K, a.V = V, a.ldkv = ldkv, a.B = B, a.off = off, a.start = start, a.rows = static_cast<int32_t>(rows);

@@ -227,7 +227,7 @@ int mx_linear_check(const char* who, int64_t M, int64_t K, const void* Wq, size_
   DLLAVA_REQUIRE(M >= 0 && M <= 0x7fffffffLL, DLLAVA_EINVAL, "%s: M = %lld", who, (long long)M);
   DLLAVA_REQUIRE(K > 0 && K % kMxBlock == 0 && K < (1 << 23), DLLAVA_ESHAPE, "%s: K must be a positive multiple of 32 below 2^23 (got %lld)", who,
                  (long long)K);
-  DLLAVA_REQUIRE(N >= 0 && N % 8 == 0 && N <= 0x7fffffffLL - 512, DLLAVA_ESHAPE, "%s: N must be a multiple of 8 (got %lld)", who, (long long)N);
+  DLLAVA_REQUIRE(N >= 0 && N % 8 == 0 && N < (1 << 27), DLLAVA_ESHAPE, "%s: N must be a multiple of 8 below 2^27 (got %lld)", who, (long long)N);
   DLLAVA_REQUIRE(act >= 0 && act <= 2, DLLAVA_EINVAL, "%s: act = %d", who, act);
   DLLAVA_REQUIRE(ldy >= N && ldy % 8 == 0, DLLAVA_EINVAL, "%s: ldy = %lld must be at least N and a multiple of 8", who, (long long)ldy);
   if (M == 0 || N == 0) return DLLAVA_OK;

@@ -80,7 +80,8 @@ int check(const char* who, const void* x, int64_t ldx, int64_t M, int64_t K, con
   DLLAVA_REQUIRE(aligned(x, 16) && aligned(packed, 256), DLLAVA_EINVAL, "%s: rows must be 16-byte, the packed buffer 256-byte aligned", who);
   DLLAVA_REQUIRE(packed_bytes >= dllava_mx_bytes(M, K), DLLAVA_ECAPACITY, "%s: the packed buffer needs %zu bytes (got %zu)", who,
                  dllava_mx_bytes(M, K), packed_bytes);
-  DLLAVA_REQUIRE(ceil_div(M, kMxTile) * (mx_padded(K) / kMxWindow) <= 0x7fffffffLL, DLLAVA_ESHAPE, "%s: too many rows", who);
+  DLLAVA_REQUIRE(ceil_div(M, kMxTile) * (mx_padded(K) / kMxWindow) < (1 << 24), DLLAVA_ESHAPE,
+                 "%s: ceil(M / 16) * ceil(K / 512) must be below 2^24", who);
   return DLLAVA_OK;
 }
 

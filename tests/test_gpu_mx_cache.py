@@ -119,6 +119,29 @@ def test_store_beyond_the_capacity():
     assert torch.nonzero(empty)[:, 0].tolist() == [*range(32, 40), *range(52, 60)]
 
 
+@pytest.mark.parametrize("B", [64, 65, 130, 4200])
+def test_store_and_load_of_many_sequences(B):
+    """More sequences than are looked through at once, most of them short, some empty, also the first and the last."""
+    rs = np.random.default_rng(B)
+    lens, start = rs.integers(0, 4, B), rs.integers(0, 15, B)
+    lens[[0, 1, B - 1]] = 0
+    lens[B // 2] = 18
+    s = Path(rs, B, 3, 1, 64)
+    off, rows = np.cumsum([0, *lens]), int(lens.sum())
+    kv = [dev(rs.standard_normal((rows, 64))).bfloat16() for _ in range(2)]
+    P.dllava_mx_cache_store(kv[0], kv[1], 64, B, i32(off), i32(start), rows, None, None, s.cache, s.err, P.BF16)
+    K, V = (f64(t).reshape(-1, 1, 64) for t in kv)
+    for b in range(B):
+        for i in range(lens[b]):
+            s.ref.put(b, start[b] + i, K[off[b] + i], V[off[b] + i])
+        s.ref.lens[b] = start[b] + lens[b]
+    s.same()
+    out = [torch.full_like(t, 9.0) for t in kv]
+    P.dllava_mx_cache_load(s.cache, B, i32(off), i32(start), rows, *out, 64, P.BF16)
+    for t, x in zip(out, (K, V)):
+        assert np.array_equal(f64(t), R.dequantize(*R.quantize(x[:, 0])))
+
+
 def test_store_of_nothing_sets_the_lengths():
     rs = np.random.default_rng(2)
     s = Path(rs, 3, 2, 1, 64)
@@ -183,6 +206,36 @@ def test_decode_long_sequence():
     ws = workspace(s, 8)
     step_and_check(s, rs, 8, ws, keep=[1, 1])
     step_and_check(s, rs, 8, ws, keep=[0, 1], scale=1.0)     # sharp softmax: the reference moves
+
+
+@pytest.mark.parametrize("splits", [0, 1, 7])
+@pytest.mark.parametrize("B,H,G,Dh", [(70, 2, 2, 64), (300, 2, 1, 64), (130, 5, 17, 64)])
+def test_decode_many_sequences(B, H, G, Dh, splits):
+    """More sequences than lanes, and units than blocks; lengths of zero to five steps."""
+    rs = np.random.default_rng(B)
+    s = Path(rs, B, 9, H, Dh)
+    s.fill(rs, rs.choice([0, 0, 1, 2, 15, 16, 17, 33, 140], B))
+    ws = workspace(s, H * G)
+    P.dllava_set_launch_override(P.LAUNCH_DECODE_SPLITS, splits)
+    try:
+        for _ in range(2):
+            step_and_check(s, rs, H * G, ws)
+    finally:
+        P.dllava_set_launch_override(P.LAUNCH_DECODE_SPLITS, 0)
+
+
+@pytest.mark.parametrize("lens,H,G", [([20000], 1, 4), ([17, 12000, 9000], 1, 16), ([40, 20000, 0, 500], 1, 1), ([6000, 6100], 4, 2)])
+def test_decode_units_of_many_blocks(lens, H, G):
+    """Sequences long enough to be cut into up to 65 parts (H = 1: the fewest units), beside short ones."""
+    rs = np.random.default_rng(sum(lens))
+    s = Path(rs, len(lens), max(lens) // 16 + 1, H, 64)
+    rows = sum(lens)
+    k, v = (dev(rs.standard_normal((rows, H, 64))).bfloat16() for _ in range(2))
+    P.dllava_mx_cache_store(k, v, H * 64, len(lens), i32(np.cumsum([0] + lens)), None, rows, None, None, s.cache, s.err, P.BF16)
+    s.ref.pages, s.ref.lens = s.pages.cpu().numpy(), np.asarray(lens, np.int64)   # (the store's bytes are tested above)
+    ws = workspace(s, H * G)
+    for _ in range(2):
+        step_and_check(s, rs, H * G, ws, keep=[1] * len(lens))
 
 
 def test_decode_at_capacity():

@@ -100,7 +100,8 @@ REFUSED = [
     ("dllava_mx_linear", EINVAL, dict(xq=C.c_void_p(0x10010))), ("dllava_mx_linear", EINVAL, dict(Wq=C.c_void_p(0x10010))),
     ("dllava_mx_linear", EINVAL, dict(bias=ODD)), ("dllava_mx_linear", EINVAL, dict(residual=ODD)), ("dllava_mx_linear", EINVAL, dict(y=ODD)),
     ("dllava_mx_linear_few", ESHAPE, dict(M=65)), ("dllava_mx_linear_few", EINVAL, dict(M=-1)), ("dllava_mx_linear_few", EINVAL, dict(ldx=60)),
-    ("dllava_mx_linear_few", EINVAL, dict(ldx=68)), ("dllava_mx_linear_few", ESHAPE, dict(ldx=1 << 24)), ("dllava_mx_linear_few", ENULL, dict(x=None)), ("dllava_mx_linear_few", EINVAL, dict(x=ODD)),
+    ("dllava_mx_linear_few", EINVAL, dict(ldx=68)), ("dllava_mx_linear_few", ESHAPE, dict(ldx=1 << 24)), ("dllava_mx_linear_few", ESHAPE, dict(N=1 << 27, ldy=1 << 27)),
+    ("dllava_mx_linear_few", ENULL, dict(x=None)), ("dllava_mx_linear_few", EINVAL, dict(x=ODD)),
     ("dllava_mx_linear_few", ECAPACITY, dict(wb=4096)), ("dllava_mx_linear_few", EDTYPE, dict(dtype=0)),
     ("dllava_mx_cache_store", EDTYPE, dict(dtype=2)), ("dllava_mx_cache_store", EDTYPE, dict(cache=_cache(1))), ("dllava_mx_cache_store", ENULL, dict(cache=None)),
     ("dllava_mx_cache_store", ESHAPE, dict(cache=_cache(Dh=96))), ("dllava_mx_cache_store", ESHAPE, dict(cache=_cache(page=32))),
@@ -108,6 +109,7 @@ REFUSED = [
     ("dllava_mx_cache_store", EINVAL, dict(ldkv=132)), ("dllava_mx_cache_store", ENULL, dict(off=None)), ("dllava_mx_cache_store", ENULL, dict(V=None)),
     ("dllava_mx_cache_store", ENULL, dict(so=FAKE)), ("dllava_mx_cache_store", ENULL, dict(si=FAKE)), ("dllava_mx_cache_store", EINVAL, dict(B=-1)),
     ("dllava_mx_cache_store", EINVAL, dict(rows=-1)), ("dllava_mx_cache_store", ESHAPE, dict(rows=1 << 31)),
+    ("dllava_mx_cache_store", ESHAPE, dict(rows=1 << 28)), ("dllava_mx_cache_store", ESHAPE, dict(B=1 << 23)), ("dllava_mx_quantize", ESHAPE, dict(M=1 << 28, bytes=1 << 40)),
     ("dllava_mx_cache_store", EINVAL, dict(start=C.c_void_p(0x30000))), ("dllava_mx_cache_store", EINVAL, dict(start=C.c_void_p(0x30004))),
     ("dllava_mx_cache_store", EINVAL, dict(start=C.c_void_p(0x2FFFC))), ("dllava_mx_cache_store", ESHAPE, dict(cache=_cache(mp=1 << 30))),
     ("dllava_mx_cache_load", EDTYPE, dict(dtype=3)), ("dllava_mx_cache_load", EDTYPE, dict(cache=_cache(0))), ("dllava_mx_cache_load", ENULL, dict(K=None)),
