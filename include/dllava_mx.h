@@ -109,6 +109,7 @@ size_t dllava_mx_decode_workspace(int32_t B, int32_t Hq, int32_t H, int32_t Dh, 
  *   O[i,h] = softmax_{j <= i}(scale * Q[i,h] . K[j,g]) V[j,g]      (rows of other sequences take no part)
  *   Q [rows, Hq, Dh] row stride ldq, K, V [rows, Hkv, Dh] row stride ldkv (elements; a fused projection's output can be passed as it is:
  *   ldq = ldkv = (Hq + 2 Hkv) * Dh), O [rows, Hq, Dh] contiguous, out; only rows < off[B] are written.  off, rows as in dllava_prefill_attn.
+ * Scores, softmax statistics and sums are float32; with DLLAVA_BF16 probabilities are rounded to bfloat16 before they meet the values.
  * Sizes: Dh in {64, 128}, Hq % Hkv == 0, row strides in multiples of 16 bytes, a row of K or V at most 2^27 bytes.  dtype DLLAVA_F32 or DLLAVA_BF16.
  */
 int dllava_group_prefill_attn(const void* Q, int64_t ldq, const void* K, const void* V, int64_t ldkv, int32_t B, const int32_t* off, int64_t rows,

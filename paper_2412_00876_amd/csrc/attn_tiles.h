@@ -27,6 +27,8 @@
 // products for heads of 128 (2900-row sequences 436 us, among the products 450), among them for heads of 64.
 // Tried and not kept: blocks of eight waves (256 queries per K/V tile: 458 against 448 us), the loads dealt out one by one (465), items
 // ordered so that a die's blocks share sequences (435 against 424 in rows).
+// With grouped heads a probability is one rounded bfloat16, so a tile has 16 products and 81 slots, and the block's part stands in front of the
+// products for both sizes of heads: 4 x 3000 rows, 32 heads of 128 over 8, 434 us in two parts, 340 in one (870 TFLOP/s; 16000 rows 1060).
 // Measured against the forms before it (products, softmax and products one after the other; for masks two groups of 16 queries with
 // 16x16x32 products): 4 sequences of 2888..3085 rows, 32 heads of 128, pages 500 -> 428 us; 16 of 158..355 rows 43.3 -> 38.2;
 // masked, 8 of 619..816 rows 111 -> 84; unmasked, 4 spans of 2880, 8 heads of 64 138 -> 120.
@@ -218,16 +220,16 @@ __device__ __forceinline__ u32x4 join(const u32x2& a, const u32x2& b) { return u
 struct Places {
   int stage[32], pair[32], at[32];
 };
-constexpr Places make_places(int first, int all, int half0, int half1) {
+constexpr Places make_places(int first, int all, int half0, int half1, int parts) {
   Places r{};
-  constexpr int w[4] = {2, 4, 3, 5};  // issue slots of a stage
+  const int w[4] = {2, 4, parts == 2 ? 3 : 1, parts == 2 ? 5 : 2}, slots_all = parts == 2 ? 112 : 72;  // issue slots of a stage, of all
   int n = 0, slots = 0;
   for (int pass = 0; pass < 4; pass += 2)
     for (int s = 0; s < 8 + 1; ++s)
       for (int st = pass + 1; st >= pass; --st) {
         const int p = s - (st - pass);
         if (p < 0 || p > 7) continue;
-        int at = all > first ? first + slots * (all - first) / 112 : first;
+        int at = all > first ? first + slots * (all - first) / slots_all : first;
         const int least = st < 2 ? 0 : (p < 4 ? half0 : half1);
         if (all > first && at < least) at = least < all ? least : all - 1;
         r.stage[n] = st, r.pair[n] = p, r.at[n] = at;
@@ -264,15 +266,17 @@ __device__ __forceinline__ void first_reference(State<DH>& T, const f32x16& S, f
 // request_k() (of later tiles) -- is called among the products, mask(S) once the scores have been written.
 // kb / vb, set by open(): LDS addresses of this lane's pieces of K(t+1) and V(t).
 // FIRST: the item's first tile (no P(t-1), the reference still at its floor).
-template <int DH, bool FIRST, bool QK, typename Open, typename Mask, typename RequestV, typename RequestK>
+// PARTS: bfloat16 parts of a probability.  Two (16 bits of it); or one, rounded: a third of the products less, and each probability off by
+// 2^-8 of itself at most, which the sum over keys averages out below the output's own rounding to the same eight bits.
+template <int DH, int PARTS, bool FIRST, bool QK, typename Open, typename Mask, typename RequestV, typename RequestK>
 __device__ __forceinline__ void step(State<DH>& T, f32x16& S, f32x16& Sn, Probs& P, const uint32_t& kb, const uint32_t& vb, float scale_log2,
                                      Open&& open, Mask&& mask, RequestV&& request_v, RequestK&& request_k) {
   constexpr int kNB = DH / 32, kKS = DH / 16, kRowBytes = DH * 2;
-  constexpr int kNP = FIRST ? 0 : kNB * 4, kNQ = QK ? kKS : 0, kNM = kNP + kNQ;
-  constexpr int kHead = FIRST ? 0 : 5;       // products in front of the probabilities
-  constexpr bool kUpFront = DH == 128;       // open and request in front of the products
-  constexpr int kReadK = kUpFront ? 0 : 2, kRequest = 4;  // products behind which K is read (two pieces each), requests are made
-  constexpr int kHaveK = DH == 128 ? 9 : 6;  // K has been read
+  constexpr int kNP = FIRST ? 0 : kNB * 2 * PARTS, kNQ = QK ? kKS : 0, kNM = kNP + kNQ;
+  constexpr int kHead = FIRST ? 0 : (PARTS == 2 ? 5 : 4);  // products in front of the probabilities
+  constexpr bool kUpFront = DH == 128 || PARTS == 1;       // open and request in front of the products
+  constexpr int kReadK = kUpFront ? 0 : 2, kRequest = 4;   // products behind which K is read (two pieces each), requests are made
+  constexpr int kHaveK = PARTS == 1 ? kNP - 1 : (DH == 128 ? 9 : 6);  // K has been read
   auto read_k = [&](auto I) DLLAVA_INLINE { T.k[I.value] = lds_read16_acc<0>(kb ^ (I.value * 32)); };
   auto read_v = [&](auto I) DLLAVA_INLINE {  // piece I of 4*kNB, ordered half, block, 8-key part
     constexpr int half = I.value / (2 * kNB), nb = (I.value / 2) % kNB, part = I.value % 2;
@@ -285,15 +289,15 @@ __device__ __forceinline__ void step(State<DH>& T, f32x16& S, f32x16& Sn, Probs&
   auto product = [&](auto Mi) DLLAVA_INLINE {
     constexpr int m = decltype(Mi)::value;
     if constexpr (m < kNP) {
-      constexpr int half = m / (2 * kNB), nb = (m / 2) % kNB;
-      pv(T.o[nb], join(T.v[nb][half][0], T.v[nb][half][1]), m % 2 == 0 ? P.hi[half] : P.lo[half]);
+      constexpr int half = m / (PARTS * kNB), nb = (m / PARTS) % kNB;
+      pv(T.o[nb], join(T.v[nb][half][0], T.v[nb][half][1]), m % PARTS == 0 ? P.hi[half] : P.lo[half]);
       if constexpr (!kUpFront && m == kReadK - 1) open();
       if constexpr (QK && m >= kReadK && m < kReadK + kKS / 2) {
         read_k(std::integral_constant<int, 2 * (m - kReadK)>{});
         read_k(std::integral_constant<int, 2 * (m - kReadK) + 1>{});
       }
       if constexpr (QK && m == kHaveK) k_here();
-      if constexpr (m > kHaveK - (DH == 64) && m <= kHaveK - (DH == 64) + kNB) {  // V's first half is used up
+      if constexpr (PARTS == 2 && m > kHaveK - (DH == 64) && m <= kHaveK - (DH == 64) + kNB) {  // V's first half is used up
         constexpr int i = 2 * (m - kHaveK + (DH == 64) - 1);
         read_v(std::integral_constant<int, i>{});
         read_v(std::integral_constant<int, i + 1>{});
@@ -304,6 +308,8 @@ __device__ __forceinline__ void step(State<DH>& T, f32x16& S, f32x16& Sn, Probs&
       if constexpr (FIRST) {
         read_v(std::integral_constant<int, 4 * ks * kNB / kKS>{});
         read_v(std::integral_constant<int, 4 * ks * kNB / kKS + 1>{});
+      } else if constexpr (PARTS == 1) {
+        if constexpr (ks < kNB) static_for<4>([&](auto I) DLLAVA_INLINE { read_v(std::integral_constant<int, 4 * ks + decltype(I)::value>{}); });
       } else if constexpr (ks >= 1 && ks <= kNB) {
         read_v(std::integral_constant<int, 2 * kNB + 2 * (ks - 1)>{});
         read_v(std::integral_constant<int, 2 * kNB + 2 * (ks - 1) + 1>{});
@@ -339,14 +345,14 @@ __device__ __forceinline__ void step(State<DH>& T, f32x16& S, f32x16& Sn, Probs&
     max_b();
     if constexpr (QK) k_here();
   } else {
-    // the maximum stands behind the fourth product: the scores' own last product must have been written
+    // the maximum stands behind the fourth (third) product: the scores' own last product must have been written
     static_for<kHead>([&](auto Mi) DLLAVA_INLINE {
       product(Mi);
-      if constexpr (decltype(Mi)::value == 3) {
+      if constexpr (decltype(Mi)::value == kHead - 2) {
         mask(S);
         max_a();
       }
-      if constexpr (decltype(Mi)::value == 4) max_b();
+      if constexpr (decltype(Mi)::value == kHead - 1) max_b();
       __builtin_amdgcn_sched_barrier(0);
     });
   }
@@ -360,7 +366,7 @@ __device__ __forceinline__ void step(State<DH>& T, f32x16& S, f32x16& Sn, Probs&
     move_reference(T, x);
     moved = true;
   }
-  constexpr Places places = make_places(kHead, kNM, kNP / 2 + 1, kNP + 1);
+  constexpr Places places = make_places(kHead, kNM, kNP / 2 + 1, kNP + 1, PARTS);
   float p0[8], p1[8], a0[8], a1[8], sum;
   auto op = [&](auto Oi) DLLAVA_INLINE {
     constexpr int st = places.stage[decltype(Oi)::value], p = places.pair[decltype(Oi)::value];
@@ -372,6 +378,15 @@ __device__ __forceinline__ void step(State<DH>& T, f32x16& S, f32x16& Sn, Probs&
       p0[p] = __builtin_amdgcn_exp2f(p0[p]);
       p1[p] = __builtin_amdgcn_exp2f(p1[p]);
       here(p0[p]), here(p1[p]);
+    } else if constexpr (PARTS == 1 && st == 2) {
+      uint32_t h = pack_bf16x2(p0[p], p1[p]);
+      here(h);
+      P.hi[p / 4][p % 4] = h;
+    } else if constexpr (PARTS == 1) {
+      const float pair = p0[p] + p1[p];
+      sum = p == 0 ? pair : sum + pair;
+      if constexpr (p == 7) T.l_run += sum;
+      here(p == 7 ? T.l_run : sum);
     } else if constexpr (st == 2) {
       uint32_t h = __builtin_amdgcn_perm(__float_as_uint(p1[p]), __float_as_uint(p0[p]), 0x07060302u);  // {hi16(p0), hi16(p1)}
       here(h);
@@ -401,7 +416,7 @@ __device__ __forceinline__ void step(State<DH>& T, f32x16& S, f32x16& Sn, Probs&
     __builtin_amdgcn_sched_barrier(0);
   });
   if constexpr (!QK) {  // V's rest: there was no product of K Q to read it behind
-    constexpr int from = FIRST ? 0 : 2 * kNB;
+    constexpr int from = FIRST || PARTS == 1 ? 0 : 2 * kNB;
     if constexpr (!FIRST) asm volatile("s_nop 7" ::: "memory");
     static_for<4 * kNB - from>([&](auto I) DLLAVA_INLINE { read_v(std::integral_constant<int, from + decltype(I)::value>{}); });
   }
@@ -421,13 +436,13 @@ __device__ __forceinline__ void step(State<DH>& T, f32x16& S, f32x16& Sn, Probs&
 }
 
 // The last P V of an item.
-template <int DH>
+template <int DH, int PARTS>
 __device__ __forceinline__ void finish(State<DH>& T, const Probs& P) {
   constexpr int kNB = DH / 32;
   asm volatile("s_nop 1" ::: "memory");  // plain writes of the outputs or the probabilities before a product
-  static_for<4 * kNB>([&](auto Mi) DLLAVA_INLINE {
-    constexpr int m = decltype(Mi)::value, half = m / (2 * kNB), nb = (m / 2) % kNB;
-    pv(T.o[nb], join(T.v[nb][half][0], T.v[nb][half][1]), m % 2 == 0 ? P.hi[half] : P.lo[half]);
+  static_for<2 * PARTS * kNB>([&](auto Mi) DLLAVA_INLINE {
+    constexpr int m = decltype(Mi)::value, half = m / (PARTS * kNB), nb = (m / PARTS) % kNB;
+    pv(T.o[nb], join(T.v[nb][half][0], T.v[nb][half][1]), m % PARTS == 0 ? P.hi[half] : P.lo[half]);
   });
   products_done();
   static_for<kNB>([&](auto I) DLLAVA_INLINE { tie_o(T.o[I.value]); });
@@ -447,6 +462,7 @@ enum class Mode { Paged, Rows, Full, Masked, Words, Group };
 // with its tile index, so every block takes its longest items first and the launch ends with the shortest ones.
 template <int DH, int NWQ, Mode MODE>
 __device__ __forceinline__ void attend_items(const PrefillArgs& args) {
+  constexpr int kParts = MODE == Mode::Group ? 1 : 2;
   constexpr bool kFull = MODE == Mode::Full, kList = MODE == Mode::Masked, kMasks = kList || MODE == Mode::Words, kGroup = MODE == Mode::Group;
   // the arguments as locals (the closures below then capture plain values, which the compiler keeps in registers)
   const int aB = args.B;
@@ -947,7 +963,7 @@ __device__ __forceinline__ void attend_items(const PrefillArgs& args) {
     // take turns; a loop that can be left in its middle, or entered there, makes the compiler move accumulators.)
     if (t <= last) {
       if ((last - t) & 1) {  // an even number of tiles
-        step<DH, true, true>(T, SA, SB, P2, kb, vb, aScale, open, any_mask, open_v, open_k);
+        step<DH, kParts, true, true>(T, SA, SB, P2, kb, vb, aScale, open, any_mask, open_v, open_k);
         ++t;
       } else {  // an odd number: pairs from the first tile on, behind products with probabilities of zero
         products_done();  // the copy reads the scores
@@ -961,16 +977,16 @@ __device__ __forceinline__ void attend_items(const PrefillArgs& args) {
         asm volatile("s_nop 1" ::: "memory");
       }
       while (t < last) {
-        step<DH, false, true>(T, SB, SA, P2, kb, vb, aScale, open, any_mask, open_v, open_k);
+        step<DH, kParts, false, true>(T, SB, SA, P2, kb, vb, aScale, open, any_mask, open_v, open_k);
         ++t;
-        step<DH, false, true>(T, SA, SB, P2, kb, vb, aScale, open, any_mask, open_v, open_k);
+        step<DH, kParts, false, true>(T, SA, SB, P2, kb, vb, aScale, open, any_mask, open_v, open_k);
         ++t;
       }
-      step<DH, false, false>(T, SB, SA, P2, kb, vb, aScale, open,
+      step<DH, kParts, false, false>(T, SB, SA, P2, kb, vb, aScale, open,
                              [&](f32x16& S) DLLAVA_INLINE { mask_scores(S, t, last, nC, kmask); },  // the diagonal, or the end of the sequence
                              open_v, open_k);
       ++t;
-      finish<DH>(T, P2);
+      finish<DH, kParts>(T, P2);
     }
     while (t <= lastC) {  // later waves of the block have more tiles
       open();

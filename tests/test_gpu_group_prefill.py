@@ -1,7 +1,7 @@
 """Causal attention of packed prompts with grouped heads against the oracle (float64).
 
 Tolerance of an output o = sum_j w_j v_j, with W = sum_j w_j |v_j| and A = scale * max_j sum |q| |k_j|.  bfloat16: its own rounding, 2^-8 |o|;
-probabilities split in two bfloat16 parts by cutting, off by 2^-14 at most; scores, exponentials and their sums in float32, twice
+probabilities rounded to bfloat16, off by half a step, 2^-8 of each at most: 2^-8 W; scores, exponentials and their sums in float32, twice
 (Dh + 16) 2^-23 A and 2 n 2^-23.  float32: no first two terms, and 2^-22 |o| for the last division and product."""
 import numpy as np
 import pytest
@@ -39,7 +39,7 @@ def run_and_check(lens, Hq, Hkv, Dh, dtype, fused, seed=0, extra=0, scale=None):
             want, W, A = R.attention(q, k, v, scale, causal=True)
             err = np.abs(f64(O[r0:r0 + m]) - want)
             tol = (2 * (Dh + 16) * 2.0 ** -23 * A[..., None] + 2 * m * 2.0 ** -23) * W
-            tol = tol + (2.0 ** -8 * np.abs(want) + 2.0 ** -14 * W if dtype == torch.bfloat16 else 2.0 ** -22 * np.abs(want))
+            tol = tol + (2.0 ** -8 * (np.abs(want) + W) if dtype == torch.bfloat16 else 2.0 ** -22 * np.abs(want))
             bad = ~(err <= tol)
             assert not bad.any(), (m, bad.sum(), np.argwhere(bad)[:4], err.max())
         r0 += m
@@ -71,7 +71,9 @@ def test_long_and_many():
     run_and_check([150, 20], 4, 2, 128, torch.bfloat16, True, scale=1.5)                  # sharp softmax
 
 
-def test_one_query_head_per_head_equals_prefill_attn():
+def test_one_query_head_per_head_against_prefill_attn():
+    """The same as dllava_prefill_attn's, whose probabilities have 16 bits (off by 2^-14 at most), but for both outputs' rounding and the one
+    probabilities': W <= max |v|."""
     rs = np.random.default_rng(5)
     lens, H, Dh = [300, 1, 77], 4, 128
     rows = sum(lens)
@@ -79,12 +81,9 @@ def test_one_query_head_per_head_equals_prefill_attn():
     Q, K, V = (torch.from_numpy(rs.standard_normal((rows, H, Dh))).to(DEV, torch.bfloat16) for _ in range(3))
     a, b = torch.zeros_like(Q), torch.zeros_like(Q)
     P.dllava_group_prefill_attn(Q, H * Dh, K, V, H * Dh, 3, off, rows, H, H, Dh, 0.09, a, P.BF16)
-    P.dllava_set_launch_override(P.LAUNCH_PREFILL_WAVES, 16)                              # its kernel for long sequences
-    try:
-        P.dllava_prefill_attn(Q, K, V, None, 3, off, rows, H, Dh, 0.09, b, P.BF16)
-    finally:
-        P.dllava_set_launch_override(P.LAUNCH_PREFILL_WAVES, 0)
-    assert torch.equal(a, b)
+    P.dllava_prefill_attn(Q, K, V, None, 3, off, rows, H, Dh, 0.09, b, P.BF16)
+    top = V.double().abs().amax((0, 2))[None, :, None]
+    assert ((a.double() - b.double()).abs() <= 2.0 ** -8 * (a.double().abs() + b.double().abs()) + (2.0 ** -8 + 2.0 ** -13) * top).all()
 
 
 def test_captured():
