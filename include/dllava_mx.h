@@ -14,6 +14,12 @@
  * (seven would round to eight), at least 1 and at most 252 (all values are then finite in float32 and bfloat16); an element is the nearest code to x / 2^(s - 127), ties to the even
  * code, magnitudes beyond six to six.  A block that holds an infinity or a NaN has s = 255, and every element of it reads as NaN.  Signs are
  * kept, also those of zeros.  The rounding is exact arithmetic: the same input gives the same bytes everywhere.
+ *
+ * dllava_set_launch_override here (any other value: the call picks, and 0 gives it back):
+ *   DLLAVA_LAUNCH_LINEAR_TILE     dllava_mx_linear: 8, 7, 6, 4 = 256 features x 256, 224, 192, 128 rows, 12 = 128 x 128, 2 = 64 x 32 with the
+ *                                 columns shared out; dllava_mx_linear_few: 1, 2, 3 = 16, 32, 48 features per block
+ *   DLLAVA_LAUNCH_DECODE_SPLITS   dllava_mx_decode_attn_append: blocks of the launch, at most as many as it would have
+ *   DLLAVA_LAUNCH_PREFILL_WAVES, DLLAVA_LAUNCH_PREFILL_BLOCKS   dllava_group_prefill_attn, bfloat16: as for dllava_prefill_attn's long sequences
  */
 #ifndef DLLAVA_MX_H
 #define DLLAVA_MX_H
@@ -58,7 +64,7 @@ int dllava_mx_dequantize(const void* packed, size_t packed_bytes, int64_t M, int
  *   xq  packed [M, K];  Wq  packed [N, K];  bias [N] float32 or NULL;
  *   residual [M, N] bfloat16 with y's row stride, or NULL (act 0, 1), may be y itself;  y [M, N] bfloat16, row stride ldy, out.
  * Products are exact, sums are float32, each result is rounded once.
- * Sizes: K % 32 == 0, N % 8 == 0, ldy % 8 == 0, K < 2^23, N < 2^27.  dtype: DLLAVA_BF16.  M == 0 or N == 0 is a no-op.
+ * Sizes: K % 32 == 0, N % 8 == 0, ldy % 8 == 0, K < 2^23, N < 2^27; ldy < 2^21, or ceil(N / 64) * ceil(M / 32) < 2^23.  dtype: DLLAVA_BF16.  M == 0 or N == 0 is a no-op.
  */
 int dllava_mx_linear(const void* xq, size_t xq_bytes, int64_t M, int64_t K, const void* Wq, size_t Wq_bytes, const float* bias, int64_t N,
                      int act, const void* residual, void* y, int64_t ldy, int dtype, void* stream);
@@ -96,7 +102,9 @@ int dllava_mx_cache_load(const dllava_kv_cache* cache, int32_t B, const int32_t*
  *   o[b,h] = softmax(scale * [K_cache; k_new] q[b,h]) [V_cache; v_new], the current token as given (not rounded to 4 bits); the keep
  *   decision, keep_out, err_flag and the update of cache_len as there; a kept token's k_new, v_new are stored in 4 bits.
  *   q, o [B, Hq, Dh], k_new, v_new [B, H, Dh] bfloat16, contiguous;  Hq % H == 0
- *   workspace  dllava_mx_decode_workspace(B, Hq, H, Dh, max_pages_per_seq) bytes, 256-byte aligned, zero-filled once (counters)
+ *   workspace  dllava_mx_decode_workspace(B, Hq, H, Dh, max_pages_per_seq) bytes, 256-byte aligned, zero-filled once (counters, which every
+ *              call leaves at zero).  It serves calls of any sizes that need no more bytes, one behind the other: calls that may
+ *              run at the same time, captured ones too, each need their own.
  * Scores, softmax statistics and sums are float32; probabilities are rounded to bfloat16 before they meet the values.
  */
 int dllava_mx_decode_attn_append(const void* q, const void* k_new, const void* v_new, int32_t B, int32_t Hq, const float* logits,
@@ -110,7 +118,7 @@ size_t dllava_mx_decode_workspace(int32_t B, int32_t Hq, int32_t H, int32_t Dh, 
  *   Q [rows, Hq, Dh] row stride ldq, K, V [rows, Hkv, Dh] row stride ldkv (elements; a fused projection's output can be passed as it is:
  *   ldq = ldkv = (Hq + 2 Hkv) * Dh), O [rows, Hq, Dh] contiguous, out; only rows < off[B] are written.  off, rows as in dllava_prefill_attn.
  * Scores, softmax statistics and sums are float32; with DLLAVA_BF16 probabilities are rounded to bfloat16 before they meet the values.
- * Sizes: Dh in {64, 128}, Hq % Hkv == 0, row strides in multiples of 16 bytes, a row of K or V at most 2^27 bytes.  dtype DLLAVA_F32 or DLLAVA_BF16.
+ * Sizes: Dh in {64, 128}, Hq % Hkv == 0, row strides in multiples of 16 bytes, a row at most 2^27 bytes, rows < 2^31 (float32: 2^24).  dtype DLLAVA_F32 or DLLAVA_BF16.
  */
 int dllava_group_prefill_attn(const void* Q, int64_t ldq, const void* K, const void* V, int64_t ldkv, int32_t B, const int32_t* off, int64_t rows,
                               int32_t Hq, int32_t Hkv, int32_t Dh, float scale, void* O, int dtype, void* stream);

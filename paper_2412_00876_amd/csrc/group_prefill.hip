@@ -20,6 +20,7 @@ __global__ __launch_bounds__(NWQ * kWave, NWQ < 4 ? 1 : 2) void group_tiles_kern
 template <int DH, int NWQ>
 int launch(const PrefillArgs& a, int64_t rows, hipStream_t st) {
   static std::atomic<int64_t> blocks{0};
+  if (a.B > kWave && (ceil_div(rows, NWQ * 32) + a.B) * a.H * (NWQ * kWave) > 0xffffffffLL) return 1;  // (a block to an item: threads of a launch)
   return launch_items(group_tiles_kernel<DH, NWQ>, NWQ, blocks, "group_tiles_kernel", a, rows, st);
 }
 
@@ -103,6 +104,7 @@ extern "C" int dllava_group_prefill_attn(const void* Q, int64_t ldq, const void*
   a.q_row_bytes = static_cast<uint32_t>(ldq * es), a.kv_row_bytes = static_cast<uint32_t>(ldkv * es);
   a.scale_log2 = scale * 1.44269504088896340736f;
   hipStream_t st = static_cast<hipStream_t>(stream);
+  DLLAVA_REQUIRE(dtype == DLLAVA_BF16 || rows < (1 << 24), DLLAVA_ESHAPE, "group_prefill: DLLAVA_F32 takes fewer than 2^24 rows");
   if (dtype == DLLAVA_F32) return Dh == 128 ? launch_f32<128>(a, rows, st) : launch_f32<64>(a, rows, st);
   const int rc = Dh == 128 ? launch_waves<128>(a, rows, st) : launch_waves<64>(a, rows, st);
   DLLAVA_REQUIRE(rc <= 0, DLLAVA_ESHAPE, "group_prefill: too many rows or sequences");

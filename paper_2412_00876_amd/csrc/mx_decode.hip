@@ -696,7 +696,8 @@ int64_t blocks_of(int64_t units, int64_t max_pages) {
   const int64_t g = ceil_div(units * (max_pages / 2 + 1), kMinShare);
   return g > kBlocksMax ? kBlocksMax : g;
 }
-size_t counter_bytes(int64_t blocks) { return static_cast<size_t>(blocks + kReadCounters + 1) * kCnt * sizeof(int32_t); }
+// Counters lie where no other call, of whatever sizes, has parts: a workspace serves calls of different sizes in turn.
+constexpr size_t kCounterBytes = static_cast<size_t>(kBlocksMax + kReadCounters + 1) * kCnt * sizeof(int32_t);
 
 }  // namespace
 }  // namespace dllava
@@ -707,7 +708,7 @@ extern "C" size_t dllava_mx_decode_workspace(int32_t B, int32_t Hq, int32_t H, i
   if (B <= 0 || H <= 0 || Hq <= 0 || Hq % H != 0 || Dh <= 0 || max_pages_per_seq <= 0) return 256;
   const int group = Hq / H;
   const int64_t blocks = blocks_of(static_cast<int64_t>(B) * H * tiles_of(group), max_pages_per_seq);
-  return round_up(counter_bytes(blocks) + static_cast<size_t>(blocks) * 2 * (group < kHeads ? group : kHeads) * (Dh + 2) * sizeof(float), 256);
+  return round_up(kCounterBytes + static_cast<size_t>(blocks) * 2 * (group < kHeads ? group : kHeads) * (Dh + 2) * sizeof(float), 256);
 }
 
 extern "C" int dllava_mx_decode_attn_append(const void* q, const void* k_new, const void* v_new, int32_t B, int32_t Hq, const float* logits,
@@ -742,7 +743,7 @@ extern "C" int dllava_mx_decode_attn_append(const void* q, const void* k_new, co
   if (const int v = launch_override(DLLAVA_LAUNCH_DECODE_SPLITS)) blocks = v < most ? v : most;  // tests: fewer blocks, larger shares
   a.cnt_read = static_cast<int32_t*>(workspace);
   a.cnt_done = a.cnt_read + (kReadCounters + 1) * kCnt;
-  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + counter_bytes(most));
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kCounterBytes);
   a.o = static_cast<bf16_t*>(o), a.keep_out = keep_out, a.err_flag = err_flag;
   const dim3 grid(static_cast<unsigned>(blocks));
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -248,7 +248,7 @@ __global__ __launch_bounds__(kSplitWaves* kWave) void mx_split_kernel(MxLinearAr
 template <int FT, int RT>
 int launch_split(const MxLinearArgs& a, hipStream_t st) {
   const int64_t n_ft = ceil_div(a.N, 16 * FT), blocks = n_ft * ceil_div(a.M, 16 * RT);
-  DLLAVA_REQUIRE(blocks <= 0x7fffffffLL, DLLAVA_ESHAPE, "mx_linear: too many results");
+  DLLAVA_REQUIRE(blocks < (1 << 23), DLLAVA_ESHAPE, "mx_linear: too many results for rows of y that far apart");
   hipLaunchKernelGGL((mx_split_kernel<FT, RT>), dim3(static_cast<unsigned>(blocks)), dim3(kSplitWaves * kWave), 0, st, a, static_cast<int>(n_ft));
   DLLAVA_CHECK_LAUNCH("mx_split_kernel");
   return DLLAVA_OK;

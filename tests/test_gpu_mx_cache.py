@@ -278,6 +278,17 @@ def test_decode_nan_stays_with_its_sequence_and_head():
     assert nan[0, 2:, :32].all() and not nan[0, :2].any() and not nan[1].any()
 
 
+def test_decode_one_workspace_for_calls_of_many_sizes():
+    """A batch that shrinks and grows, other heads and other caches, on one workspace of the largest call's size."""
+    rs = np.random.default_rng(15)
+    paths = [(Path(rs, B, mp, H, Dh), Hq) for B, mp, H, Dh, Hq in ((1, 3, 1, 64, 4), (40, 40, 2, 64, 8), (3, 60, 4, 128, 4), (70, 5, 1, 64, 16))]
+    for s, _ in paths:
+        s.fill(rs, rs.integers(0, s.cap - 2, s.B))
+    ws = torch.zeros(max(workspace(s, Hq).numel() for s, Hq in paths), dtype=torch.uint8, device=DEV)
+    for i in (0, 1, 2, 1, 3, 0, 2):
+        step_and_check(*paths[i][:1], rs, paths[i][1], ws)
+
+
 def test_decode_captured_and_on_another_stream():
     rs = np.random.default_rng(12)
     s, t = Path(rs, 5, 8, 2, 128, junk=0), None

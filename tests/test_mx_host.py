@@ -126,6 +126,8 @@ REFUSED = [
     ("dllava_group_prefill_attn", ESHAPE, dict(Hkv=0)), ("dllava_group_prefill_attn", EINVAL, dict(ldq=192)), ("dllava_group_prefill_attn", EINVAL, dict(ldkv=132)),
     ("dllava_group_prefill_attn", ESHAPE, dict(ldkv=(1 << 26) + 8)), ("dllava_group_prefill_attn", EINVAL, dict(scale=-1.0)),
     ("dllava_group_prefill_attn", ENULL, dict(K=None)), ("dllava_group_prefill_attn", EINVAL, dict(V=ODD)), ("dllava_group_prefill_attn", ENULL, dict(off=None)),
+    ("dllava_group_prefill_attn", ESHAPE, dict(rows=1 << 24, dtype=0)),
+    ("dllava_group_prefill_attn", ESHAPE, dict(rows=0x7fffffff, B=65, dtype=1)),
     ("dllava_group_prefill_attn", EINVAL, dict(rows=-1)), ("dllava_group_prefill_attn", ESHAPE, dict(rows=1 << 31)), ("dllava_group_prefill_attn", EINVAL, dict(B=-2)),
 ]
 
