@@ -28,7 +28,8 @@
 // Tried and not kept: blocks of eight waves (256 queries per K/V tile: 458 against 448 us), the loads dealt out one by one (465), items
 // ordered so that a die's blocks share sequences (435 against 424 in rows).
 // With grouped heads a probability is one rounded bfloat16, so a tile has 16 products and 81 slots, and the block's part stands in front of the
-// products for both sizes of heads: 4 x 3000 rows, 32 heads of 128 over 8, 434 us in two parts, 340 in one (870 TFLOP/s; 16000 rows 1060).
+// products for both sizes of heads: 4 x 3000 rows, 32 heads of 128 over 8, 434 us in two parts, 340 in one, 314 with the heads dealt to
+// the dies (940 TFLOP/s; 16000 rows 1050).
 // Measured against the forms before it (products, softmax and products one after the other; for masks two groups of 16 queries with
 // 16x16x32 products): 4 sequences of 2888..3085 rows, 32 heads of 128, pages 500 -> 428 us; 16 of 158..355 rows 43.3 -> 38.2;
 // masked, 8 of 619..816 rows 111 -> 84; unmasked, 4 spans of 2880, 8 heads of 64 138 -> 120.
@@ -453,6 +454,11 @@ __device__ __forceinline__ void finish(State<DH>& T, const Probs& P) {
 // Group: causal, in rows, several query heads to a head of K and V, rows of any stride.
 enum class Mode { Paged, Rows, Full, Masked, Words, Group };
 
+// Which of a tile's grouped query heads comes i-th: a die (every eighth block) takes neighbours, which share keys and values in its cache (4 x
+// 3000 rows, 32 heads of 128 over 8: 336 -> 314 us, and 294 MB are fetched instead of 1340).
+constexpr int kDies = 8;
+__device__ __forceinline__ int head_of(int i, int heads) { return heads % kDies == 0 ? i % kDies * (heads / kDies) + i / kDies : i; }
+
 // One work item = (sequence, head, tile of NWQ*32 query rows).  Blocks are PERSISTENT: the launch holds as many blocks as
 // fit the chip at once (slots), block p takes every slots-th item and walks their key tiles as ONE stream: the tile
 // loads run two tiles ahead of the arithmetic across item boundaries, and the queries of the next item go to LDS while
@@ -558,6 +564,7 @@ __device__ __forceinline__ void attend_items(const PrefillArgs& args) {
     Item it{0, 0, 0, 0, 0, 0, -1};
     const int heads = arg(&PrefillArgs::H), yd = k / heads;  // position in DESCENDING tile-index order
     it.h = k - yd * heads;
+    if constexpr (kGroup) it.h = head_of(it.h, heads);
     const int y = total - 1 - yd;  // position in ascending order
     if (y < 0) return it;          // (total is 0 for more sequences: those have one item per block)
     int below = 0, tile = 0;       // tiles with a smaller index
@@ -589,7 +596,11 @@ __device__ __forceinline__ void attend_items(const PrefillArgs& args) {
   // (sorted by descending work) in alternating directions, so a block that got a longer item in one round gets a
   // shorter one in the next and the blocks' totals stay close (C5 shape: 40..42 tiles per block instead of 36..46).
   const int pblk = static_cast<int>(blockIdx.x);
-  auto item_of = [&](int j) __attribute__((always_inline)) { return ((j & 1) ? step_blocks - 1 - pblk : pblk) + j * step_blocks; };
+  auto item_of = [&](int j) __attribute__((always_inline)) {
+    if constexpr (kGroup)  // (in eights, so that a die keeps its heads)
+      if (step_blocks % kDies == 0) return ((j & 1) ? step_blocks - kDies - pblk + 2 * (pblk % kDies) : pblk) + j * step_blocks;
+    return ((j & 1) ? step_blocks - 1 - pblk : pblk) + j * step_blocks;
+  };
   int jC = 0;
   Item C{0, 0, 0, 0, 0, 0, -1};
   if (by_lane) {
@@ -606,7 +617,7 @@ __device__ __forceinline__ void attend_items(const PrefillArgs& args) {
       if (past) {
         const int l = __builtin_ctzll(past);
         // the sequence's first tile is number upto - nt, its last upto - 1: counted from the last
-        C = {1, b0 + l, pblk % H, __builtin_amdgcn_readlane(upto, l) - 1 - tile, __builtin_amdgcn_readlane(r0, l), __builtin_amdgcn_readlane(n, l), -1};
+        C = {1, b0 + l, kGroup ? head_of(pblk % H, H) : pblk % H, __builtin_amdgcn_readlane(upto, l) - 1 - tile, __builtin_amdgcn_readlane(r0, l), __builtin_amdgcn_readlane(n, l), -1};
         C.seen = seen_before(C);
         break;
       }

@@ -2,9 +2,9 @@
 // of any stride.
 //
 // bfloat16: the matrix-core kernel of attn_tiles.h.  What it takes per item (one query head, NWQ * 32 query rows) does not depend on
-// whose keys it reads; the query heads of a group are neighbours in the order of the items, so that their K/V tiles are read from the
-// caches.  The probabilities are rounded to bfloat16 (nearest) for the second product, as those of the decode steps over the cache in
-// 4 bits are; their sum is taken before.  Bound by the matrix cores: 4 x 3000 rows, 32 query heads of 128 over 8, 340 us, 870 TFLOP/s.
+// whose keys it reads; the query heads of a group run on one die at about the same time (where eight divides their number), so that
+// their K/V tiles come from its cache.  The probabilities are rounded to bfloat16 (nearest) for the second product, as those of the decode steps over the cache in
+// 4 bits are; their sum is taken before.  Bound by the matrix cores: 4 x 3000 rows, 32 query heads of 128 over 8, 314 us, 940 TFLOP/s.
 // float32: the wave-level streaming attention of attend.h, one wave per row and query head.
 #include "attend.h"
 #include "attn_tiles.h"

@@ -46,19 +46,21 @@ def run_and_check(lens, Hq, Hkv, Dh, dtype, fused, seed=0, extra=0, scale=None):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("Hq,Hkv,Dh", [(1, 1, 64), (4, 2, 128), (7, 1, 64), (14, 2, 64), (8, 8, 128), (6, 1, 128)])
+@pytest.mark.parametrize("Hq,Hkv,Dh", [(1, 1, 64), (4, 2, 128), (7, 1, 64), (14, 2, 64), (8, 8, 128), (6, 1, 128), (24, 4, 64), (16, 2, 128)])
 @pytest.mark.parametrize("fused", [False, True])
 def test_ragged(Hq, Hkv, Dh, dtype, fused):
     run_and_check([5, 0, 1, 16, 33, 64, 0, 127, 130, 1], Hq, Hkv, Dh, dtype, fused)
 
 
+@pytest.mark.parametrize("blocks", [3, 16])
 @pytest.mark.parametrize("waves", [1, 2, 4])
 @pytest.mark.parametrize("Dh", [64, 128])
-def test_every_launch_shape(Dh, waves):
+def test_every_launch_shape(Dh, waves, blocks):
     P.dllava_set_launch_override(P.LAUNCH_PREFILL_WAVES, waves)
-    P.dllava_set_launch_override(P.LAUNCH_PREFILL_BLOCKS, 3)
+    P.dllava_set_launch_override(P.LAUNCH_PREFILL_BLOCKS, blocks)
     try:
         run_and_check([1, 100, 257, 31], 4, 2, Dh, torch.bfloat16, True)
+        run_and_check([1, 100, 257, 31], 8, 2, Dh, torch.bfloat16, True)
     finally:
         P.dllava_set_launch_override(P.LAUNCH_PREFILL_WAVES, 0)
         P.dllava_set_launch_override(P.LAUNCH_PREFILL_BLOCKS, 0)
@@ -67,6 +69,8 @@ def test_every_launch_shape(Dh, waves):
 def test_long_and_many():
     run_and_check([900, 3], 4, 1, 128, torch.bfloat16, False)
     run_and_check([(7 * i) % 40 for i in range(80)], 4, 2, 64, torch.bfloat16, True)      # more than 64 sequences
+    run_and_check([(5 * i) % 37 for i in range(70)], 16, 4, 64, torch.bfloat16, False)    # the same, heads in eights
+    run_and_check([1500, 700], 40, 8, 64, torch.bfloat16, True)                           # several rounds of items to a block
     run_and_check([200], 8, 2, 128, torch.bfloat16, True, extra=37)                       # rows is an upper bound
     run_and_check([150, 20], 4, 2, 128, torch.bfloat16, True, scale=1.5)                  # sharp softmax
 
