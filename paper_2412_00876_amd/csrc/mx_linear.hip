@@ -4,8 +4,8 @@
 // wave take the four bytes of the scales that lie together (see the packed form in dllava_mx.h).  The products' rate is four times that
 // of bfloat16, so nearly everything else bounds them: 16384 x 8192 x 8192 takes 487 us (4.5 PFLOP/s), where a stage of 256 x 256 x 256 takes 1.43 us
 // with random values, 1.12 with zeros (the clock gives way to the power) and 0.85 by the products' own rate; at 4096 columns a
-// tile's ends and the last round of tiles count, and what the results take to memory: 5003 x 11008 x 4096 116 us (3.9 PFLOP/s), 129 with a gate that is
-// read, 135 with GELU.
+// tile's ends and the last round of tiles count, and what the results take to memory: 5003 x 11008 x 4096 115 us (3.9 PFLOP/s), 135 with a gate that is
+// read (110 MB, as many as are written), 136 with GELU.
 #include "mx_linear.h"
 #include "mx_ring.h"
 
@@ -83,12 +83,25 @@ __global__ __launch_bounds__(kRingThreads, PER_CU) void mx_ring_kernel(MxLinearA
   // rows of lanes: a lane then has eight consecutive features of one of them (n_out + 32 p of the tile), four lanes 64 bytes of a row.
   const int n_lane = 16 * FI * (w >> 1) + 4 * g, n_out = 16 * FI * (w >> 1) + 16 * (g & 1) + 8 * (g >> 1);
   const uint32_t ld = static_cast<uint32_t>(a.ldy) * 2, lane_at = static_cast<uint32_t>(16 * JT * (w & 1) + r16) * ld + 2 * static_cast<uint32_t>(n_out);
+  // R's lines of a tile are asked for while its last products run, a line a lane every other stage, so that they are in the caches at its end:
+  // all tiles end at about the same time.  5003 rows x 4096 features x 4096 columns with a residual 60.2 -> 57.1 us, 16384 x 11008 x 4096 444 -> 435;
+  // with a gate 5003 x 11008 x 4096 140.3 -> 138.5.  (Every stage of the last ones: slower than without.  Tiles of 128 rows lose 1 %.)
+  constexpr bool kAhead = (E == kAdd || E == kGate) && JT >= 6;
+  constexpr int kLines = FI / 2, kTouches = (kTok * kLines + kRingThreads - 1) / kRingThreads;
+  const uint32_t touch_at = static_cast<uint32_t>(tid / kLines) * ld + 128 * (tid % kLines);
+  uint32_t touched = 0, touch = 0;
+  mx_buffer R = mx_make_buffer(a.R, 0);
   mx_ring_stream<FI, JT>(
       buffers(ft, rt), ga, gb, a.windows, smem, w, acc,
       [&]() DLLAVA_INLINE {
         ft = ft_next, rt = rt_next;
         local += step;
         more = find_tile(tiles, local, ft_next, rt_next);
+        if constexpr (kAhead) {
+          const int64_t m0 = static_cast<int64_t>(rt) * kTok, c0 = static_cast<int64_t>(ft) * kFeat, rows = a.M - m0 < kTok ? a.M - m0 : kTok;
+          R = mx_make_buffer(a.R + m0 * a.ldy + c0, (rows - 1) * static_cast<int64_t>(ld) + 2 * (a.N - c0));
+          touch = c0 + 64 * (tid % kLines) < a.N ? touch_at : 0x80000000u;
+        }
         const int64_t n0 = static_cast<int64_t>(ft) * kFeat + n_lane;
         static_for<FI>([&](auto I) DLLAVA_INLINE {
           if (a.bias) {
@@ -100,10 +113,19 @@ __global__ __launch_bounds__(kRingThreads, PER_CU) void mx_ring_kernel(MxLinearA
         });
         return buffers(ft_next, rt_next);  // (the tile's own where there is no other: find_tile then leaves the numbers alone)
       },
+      [&](int left) DLLAVA_INLINE {
+        if constexpr (kAhead) {
+          if (left <= kTouches) {
+            asm volatile("" ::"v"(touched));
+            touched = __builtin_amdgcn_raw_buffer_load_b32(R, touch, static_cast<uint32_t>(kTouches - left) * (kRingThreads / kLines) * ld, 0);
+          }
+        }
+      },
       [&]() DLLAVA_INLINE {
         const int64_t n0 = static_cast<int64_t>(ft) * kFeat, m0 = static_cast<int64_t>(rt) * kTok, rows = a.M - m0 < kTok ? a.M - m0 : kTok;
         const int64_t bytes = (rows - 1) * static_cast<int64_t>(ld) + 2 * (a.N - n0);  // behind the last row's end nothing is read or written
-        const mx_buffer Y = mx_make_buffer(a.Y + m0 * a.ldy + n0, bytes), R = mx_make_buffer(a.R + m0 * a.ldy + n0, bytes);
+        const mx_buffer Y = mx_make_buffer(a.Y + m0 * a.ldy + n0, bytes);
+        if constexpr (!kAhead) R = mx_make_buffer(a.R + m0 * a.ldy + n0, bytes);
         uint32_t off[FI / 2];
 #pragma unroll
         for (int p = 0; p < FI / 2; ++p) off[p] = n0 + n_out + 32 * p < a.N ? lane_at + 64 * p : 0x80000000u;  // features past N: out of range
@@ -115,6 +137,7 @@ __global__ __launch_bounds__(kRingThreads, PER_CU) void mx_ring_kernel(MxLinearA
           for (int p = 0; p < FI / 2; ++p) r[j % kDeep][p] = __builtin_amdgcn_raw_buffer_load_b128(R, off[p], 16 * j * ld, 0);
         };
         if (has_r) static_for<(kDeep < JT ? kDeep : JT)>(load_r);
+        if constexpr (kAhead) asm volatile("" ::"v"(touched));
         static_for<JT>([&](auto J) DLLAVA_INLINE {
           constexpr int j = decltype(J)::value;
           u32x4 out[FI / 2];

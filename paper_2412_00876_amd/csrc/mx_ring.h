@@ -61,10 +61,11 @@ __device__ __forceinline__ void mx_start(ring_f32x4& c, const float4& v) {
 
 // All tiles of a block.  ga[j] / gb[j]: this lane's byte offsets (row * row bytes + ring_load_chunk_bytes) for its tile loads; windows = Kp / 512 >= 1; w = wave index (wave-uniform).
 //   first: the buffers of the first tile;  begin(): a tile begins: sets acc, returns the buffers of the tile after it (or its own again)
+//   on_the_way(left): left windows of the tile are left, the one at hand included; loads made here have the time of a stage
 //   done(): the tile is complete in acc (its layout: gemm_ring_halves); returns whether there is another
-template <int FI, int JT, typename Begin, typename Done>
+template <int FI, int JT, typename Begin, typename OnTheWay, typename Done>
 __device__ __forceinline__ void mx_ring_stream(const MxTileBuffers& first, const uint32_t (&ga)[FI], const uint32_t (&gb)[JT], int windows,
-                                               DLLAVA_LDS char* smem, int w, ring_f32x4 (&acc)[FI][JT], Begin&& begin, Done&& done) {
+                                               DLLAVA_LDS char* smem, int w, ring_f32x4 (&acc)[FI][JT], Begin&& begin, OnTheWay&& on_the_way, Done&& done) {
   static_assert(JT >= 4 && JT <= FI, "a slot holds the rows of either tile");
   constexpr int kMF = FI * JT, kNR = FI + JT;
   constexpr uint32_t kStage = kRingRowBytes;  // bytes of a row
@@ -165,6 +166,7 @@ __device__ __forceinline__ void mx_ring_stream(const MxTileBuffers& first, const
 
   uint32_t o0 = 0, o1 = kS, o2 = 2 * kS, o3 = 3 * kS, o4 = 4 * kS;  // byte offsets of the slots of B(k), A(k), B(k+1), A(k+1), B(k+2)
   uint32_t ab = (a_at ^ 64u) + o1, bb = (b_at ^ 64u) + o0;
+  int left = windows;
   // one stage; P: its number in the window
   auto stage = [&](auto P) DLLAVA_INLINE {
     constexpr int p = decltype(P)::value;
@@ -182,6 +184,7 @@ __device__ __forceinline__ void mx_ring_stream(const MxTileBuffers& first, const
     kstep(va, vb, ua, ub, ab, bb, std::integral_constant<int, 2 * p + 1>{}, std::true_type{}, o0, [&](auto E) DLLAVA_INLINE {
       constexpr int m = kMF - 1 - decltype(E)::value;  // (behind product m)
       if constexpr (p == 0 && m < kNR) scale1(std::integral_constant<int, m>{});
+      if constexpr (p == 0 && m == kNR) on_the_way(left);
       if constexpr (decltype(E)::value == 4) {
         const uint32_t t0 = o0, t1 = o1;
         o0 = o2, o1 = o3, o2 = o4, o3 = t0, o4 = t1;
@@ -197,7 +200,7 @@ __device__ __forceinline__ void mx_ring_stream(const MxTileBuffers& first, const
     });
   };
   for (;;) {
-    int left = windows;
+    left = windows;
     do {
       stage(std::integral_constant<int, 0>{});
       stage(std::integral_constant<int, 1>{});
