@@ -6,7 +6,7 @@
 // waits for another, and no workspace is needed.
 //  * x goes to LDS by asynchronous loads of whole 128-byte lines, tiles of 64 columns, a ring of D of them for each wave alone (no
 //    barriers).  (Straight to registers, in the layout of the products, the same bytes took twice as long: a load then touches parts of 32
-//    lines; 37 rows x 4096 features x 11008 columns 32 us instead of 19.3, but 1 x 4096 x 4096 5.0 instead of 5.4.)
+//    lines; 37 rows x 4096 features x 11008 columns 32 us instead of 18.5.)
 //  * A lane reads 16 bytes of codes, 32 elements of one feature, which become bfloat16 in registers (exact: two significant bits times a
 //    power of two), operands of v_mfma_f32_16x16x32_bf16, whose columns are the rows of x.  A product takes eight columns of each of its
 //    four lane groups, consecutive ones in LDS; the codes are exchanged between the groups to match, four swaps for 16 features x 128.
@@ -130,19 +130,21 @@ __global__ __launch_bounds__(kWaves* kWave) void mx_few_kernel(MxLinearArgs a) {
     for (int t = 0; t < D - 1; ++t) request_x(col_of(w, t), t);
   }
   int slot_now = 0;  // of the tile at hand, where it does not follow from the tile's number
-  for (int win = w; win < a.windows; win += kWaves) {
-    const int next = win + kWaves < a.windows ? win + kWaves : win;  // (past the end: this one again, not used)
+  // One window; LAST: the wave's last one, behind which nothing is asked for.
+  auto window = [&](int win, auto LAST) __attribute__((always_inline)) {
+    constexpr bool kLast = decltype(LAST)::value;
+    const int next = win + kWaves;
 #pragma unroll
     for (int f = 0; f < FT; ++f)
 #pragma unroll
       for (int i = 0; i < 4; ++i) sc[f][i] = sc_next[f][i];
-    load_s(next);
+    if constexpr (!kLast) load_s(next);
     uint32_t words[FT][4];
-#pragma unroll
-    for (int tile = 0; tile < 8; ++tile) {
-      const int j = tile / 2, ahead = tile + D - 1, slot = kSlots ? tile % D : slot_now;
-      request_x(col_of(ahead < 8 ? win : next, ahead % 8), slot == 0 ? D - 1 : slot - 1);
-      if (tile % 2 == 0) {
+    static_for<8>([&](auto Tile) __attribute__((always_inline)) {
+      constexpr int tile = decltype(Tile)::value, j = tile / 2, ahead = tile + D - 1;
+      const int slot = kSlots ? tile % D : slot_now;
+      if constexpr (!kLast || ahead < 8) request_x(col_of(ahead < 8 ? win : next, ahead % 8), slot == 0 ? D - 1 : slot - 1);
+      if constexpr (tile % 2 == 0) {
 #pragma unroll
         for (int f = 0; f < FT; ++f) {
           // word i of lane group g: columns 8i of block g -> word i: columns 8g of block i
@@ -153,9 +155,9 @@ __global__ __launch_bounds__(kWaves* kWave) void mx_few_kernel(MxLinearArgs a) {
           words[f][0] = p01[0], words[f][1] = p01[1], words[f][2] = p23[0], words[f][3] = p23[1];
         }
       }
-      // this wave's loads of the tile have landed: RG loads of each of the D - 1 tiles behind it may be on their way (and whatever else was
+      // this wave's loads of the tile have landed: RG loads of each of the tiles asked for behind it may be on their way (and whatever else was
       // requested since, which only makes the wait longer)
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 1) * RG) : "memory");
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kLast && ahead >= 8 ? 7 - tile : D - 1) * RG) : "memory");
       ring_u32x4 x[MT][2];
       lds_read_tile<MT>(x, frag + slot * kTileBytes + (g ^ swizzle) * 16, frag + slot * kTileBytes + ((4 + g) ^ swizzle) * 16);
 #pragma unroll
@@ -168,12 +170,16 @@ __global__ __launch_bounds__(kWaves* kWave) void mx_few_kernel(MxLinearArgs a) {
           for (int t = 0; t < MT; ++t) acc[f][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv, __builtin_bit_cast(bf16x8, x[t][i]), acc[f][t], 0, 0, 0);
         }
       }
-      if (tile % 2 == 1) load_w(next, j);
-      if (!kSlots) slot_now = slot_now + 1 < D ? slot_now + 1 : 0;
-    }
+      if constexpr (!kLast && tile % 2 == 1) load_w(next, j);
+      if constexpr (!kSlots) slot_now = slot_now + 1 < D ? slot_now + 1 : 0;
+    });
+  };
+  if (w < a.windows) {
+    int win = w;
+    for (; win + kWaves < a.windows; win += kWaves) window(win, std::false_type{});
+    window(win, std::true_type{});
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (tiles requested past the end)
-  __syncthreads();                                   // the rings' memory takes the sums
+  __syncthreads();  // the rings' memory takes the sums
   // register e of acc[f][t]: feature n0 + 16 f + 4 g + e, row 16 t + r16
   float4* const sm = reinterpret_cast<float4*>(smem_raw);  // [kWaves][FT * MT][kWave]
 #pragma unroll
@@ -203,17 +209,20 @@ int launch_few(const MxLinearArgs& a, hipStream_t st) {
 template <int RG>
 int launch_rows(const MxLinearArgs& a, int ft, hipStream_t st) {
   if (ft == 1) return launch_few<1, RG>(a, st);
-  return ft == 2 ? launch_few<2, RG>(a, st) : launch_few<3, RG>(a, st);
+  if (ft == 2) return launch_few<2, RG>(a, st);
+  return launch_few<3, RG == 3 || RG == 4 ? 5 : RG>(a, st);  // (three and four groups: the registers do not suffice; rows past M cost nothing)
 }
 
-// Tiles of features per block: whole rounds of a block on each compute unit, each round 3 us, and for every 512 columns of a wave 0.6 us for eight
-// rows and 1.9 for 16 features.  Measured, one tile / two / three, in us: 1 row x 11008 features x 4096 columns 12.1 / 13.1 / 10.8, 64 rows 26.2 /
-// 23.8 / 16.6; 1 x 5120 x 13824 17.0 / 17.7 / 21.3, 64 52.5 / 33.7 / 41.0; 1 x 4096 x 4096 5.4 / 7.0 / 8.9; 37 x 4096 x 11008 19.3 / 23.6 / 28.7.
+// Tiles of features per block: whole rounds of a block on each compute unit; a round takes, for every 512 columns of a wave, 0.7 us for eight rows
+// and 1.7 for 16 features, and its start 0.8, of which little is seen where two blocks share a unit.  Measured, one tile / two / three, in us: rows x
+// features x columns 1 x 11008 x 4096 9.4 / 9.9 / 9.1, 64 24.0 / 21.4 / 15.0; 1 x 13824 x 5120 13.8 / 13.4 / 19.1, 64 39.0 / 28.1 / 33.0; 1 x 4096 x 4096 4.7 /
+// 5.8 / 7.2; 37 x 4096 x 11008 18.5 / 22.3 / 26.6; 1 x 32000 x 4096 20.9 / 18.1 / 22.9, 64 60.7 / 42.1 / 40.0.
 int pick_features(const MxLinearArgs& a, int rg) {
   int best = 1;
   int64_t best_cost = 0;
   for (int ft = 1; ft <= 3; ++ft) {
-    const int64_t rounds = ceil_div(ceil_div(a.N, 16 * ft), 256), cost = rounds * (24000 + a.windows * (600 * rg + 1900 * ft));
+    const int64_t rounds = ceil_div(ceil_div(a.N, 16 * ft), 256), start = ft <= 2 && rg <= 2 ? 800 : 6400;
+    const int64_t cost = rounds * (start + a.windows * (700 * rg + 1700 * ft));
     if (ft == 1 || cost < best_cost) best = ft, best_cost = cost;
   }
   return best;

@@ -27,7 +27,7 @@ struct PrefillArgs {
   // are not zero in front of 4i.  Behind those the visible keys as a list: entry off[b] + 32 b + r is where the row of sequence b's
   // visible key r starts, in bytes (mod 2^32) from the row of its key 0.
   int32_t mask_slots;
-  // Grouped heads (group_tiles_launch only): query heads per head of K and V, bytes from a row to the next of Q, and of K and V.
+  // Grouped heads (group_prefill.hip only): query heads per head of K and V, bytes from a row to the next of Q, and of K and V.
   int32_t group;
   uint32_t q_row_bytes, kv_row_bytes;
 };
