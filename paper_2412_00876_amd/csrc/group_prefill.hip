@@ -24,10 +24,13 @@ int launch(const PrefillArgs& a, int64_t rows, hipStream_t st) {
   return launch_items(group_tiles_kernel<DH, NWQ>, NWQ, blocks, "group_tiles_kernel", a, rows, st);
 }
 
+// Waves of an item, 32 query rows each: four, but two for short sequences as long as there are not many, whose items then start sooner and
+// spread further.  Two / four waves in us, 32 heads of 128 over 8: 4 x 128 rows 8.2 / 8.9, 8 x 128 9.1 / 9.8, 4 x 256 11.5 / 11.7, 1 x 500 15.7 / 16.3, 2 x 500 16.6 / 16.4,
+// 16 x 300 of 32 heads 50.5 / 42.3; 14 heads of 64 over 2, 9 x 0..260 8.8 / 9.4, 1 x 2000 35.5 / 34.6; 8 heads of 128, 1 x 1000 24.5 / 24.3.
 template <int DH>
 int launch_waves(const PrefillArgs& a, int64_t rows, hipStream_t st) {
   const int64_t work = rows * a.H;
-  int nwq = work >= 8 * 1024 ? 4 : (work >= 1024 ? 2 : 1);
+  int nwq = work > 32 * 1024 || rows > 400 * static_cast<int64_t>(a.B) ? 4 : (work >= 1024 ? 2 : 1);
   if (const ForcedForm forced = forced_form(launch_override(DLLAVA_LAUNCH_PREFILL_WAVES)); forced.waves) nwq = forced.waves;
   if (nwq == 4) return launch<DH, 4>(a, rows, st);
   if (nwq == 2) return launch<DH, 2>(a, rows, st);
